@@ -362,6 +362,86 @@ lynx_status lynx_partition_solve(const lynx_partition_problem* problem, int32_t*
 lynx_status lynx_policy_layer_problem(const lynx_layer_config* cfg, lynx_policy_problem* problem_out,
                                       uint32_t* parents_out, double* bytes_out);
 
+/* ---- Attention over packed sequences ---------------------------------------
+ * Causal attention of one layer's heads over a batch whose sequences stand
+ * behind one another in the token dimension, with grouped heads and, optionally,
+ * a learned relative position bias by buckets; forward and backward, without a
+ * seq x seq tensor.  For sequence s the tokens are offsets[s] <= t < offsets[s+1];
+ * query head h reads key head h / (heads / kv_heads), and with i, j of the same
+ * sequence, j <= i,
+ *   z[h,i,j]  = scale q[i,h].k[j] + table[bucket(i - j), h]
+ *   lse[h,i]  = log sum_j exp z          p = exp(z - lse)
+ *   out[i,h]  = sum_j p v[j]
+ * and for a gradient d_out, with ds = p (d_out[i,h].v[j] - d_out[i,h].out[i,h]),
+ *   d_q[i,h] = scale sum_j ds k[j]       d_table[b,h] = sum_{bucket(i-j)=b} ds
+ *   d_k[j] = scale sum_{h,i} ds q[i,h]   d_v[j] = sum_{h,i} p d_out[i,h]
+ * summed over the query heads of the key head's group.
+ *
+ * Tensors: q, out, d_out, d_q [tokens, heads, head_dim], k, v, d_k, d_v [tokens,
+ * kv_heads, head_dim], lse [heads, tokens] fp32 (dense).  Heads are adjacent
+ * (head h at column h head_dim of its token's row); the distance between tokens
+ * is a stride of the config, so that q, k and v may be columns of one fused
+ * projection, and d_q, d_k, d_v columns of its gradient.  bias_table and
+ * d_bias_table [num_buckets, heads].  out shares its stride with d_out.  Gradients
+ * are overwritten and must not overlap any input or one another's elements.
+ *
+ * offsets (device, sequences + 1 entries, not decreasing, between 0 and tokens) is
+ * read by the kernels only: lengths may change under a captured graph.  Sequences
+ * may be empty.  Rows of no sequence (before offsets[0], from offsets[sequences] on)
+ * are neither read nor written.  Entries outside 0..tokens or decreasing ones reach
+ * no memory outside the tensors, but then results are undefined.
+ *
+ * Sums are fp32; probabilities and ds are rounded to the storage type for the
+ * products they enter (not in fp32 storage, and not for d_bias_table).  Every sum has
+ * one order, whatever else runs: the same call gives the same bits.  A row of logits
+ * that are all minus infinity (a table may hold minus infinity) gives out 0, lse minus
+ * infinity and no gradient.  An infinity or NaN in q, k, v or d_out reaches the results
+ * it is a term of and no others; calls that meet one take longer.  Differences of
+ * positions from bucket_starts[num_buckets - 1] on are in the last bucket.
+ *
+ * Constraints (else LYNX_ERR_SHAPE): heads a multiple of kv_heads; head_dim a multiple
+ * of 8 up to 128; tokens <= 2^24; sequences <= 2^20; num_buckets <= 64, starts <= 4096;
+ * strides multiples of 8, at least their row, at most 2^21.  0 < scale < infinity,
+ * bucket_starts from 0 on and not decreasing (else LYNX_ERR_INVALID_ARG). */
+#define LYNX_ATTENTION_MAX_HEAD_DIM 128
+#define LYNX_ATTENTION_MAX_STRIDE (1 << 21)
+#define LYNX_MAX_BUCKETS 64
+#define LYNX_MAX_DISTANCE 4096
+typedef struct {
+  int32_t dtype;       /* lynx_dtype: storage type of every tensor but lse */
+  int32_t heads;       /* query heads */
+  int32_t kv_heads;    /* key and value heads */
+  int32_t head_dim;
+  int32_t tokens;      /* rows of every tensor */
+  int32_t sequences;
+  float scale;         /* usually 1 / sqrt(head_dim) */
+  int32_t num_buckets; /* 0: no position bias; the table pointers are then ignored */
+  const int32_t* bucket_starts; /* host, num_buckets entries: the first distance of each bucket */
+  int64_t q_stride, k_stride, v_stride, out_stride; /* elements between tokens */
+  int64_t dq_stride, dk_stride, dv_stride;          /* backward only */
+} lynx_attention_config;
+
+/* Errors: INVALID_ARG (null or misaligned pointer: 16 bytes, offsets and lse 4), SHAPE, HIP. */
+lynx_status lynx_attention_forward(const lynx_attention_config* cfg, const void* q, const void* k, const void* v,
+                                   const int32_t* offsets, const void* bias_table, void* out, float* lse,
+                                   void* hip_stream);
+
+/* Device bytes of the workspace of a backward pass; 0 on a bad config. */
+size_t lynx_attention_backward_bytes(const lynx_attention_config* cfg);
+
+/* out and lse are those of the forward call.  workspace: 256-byte aligned, free for any use before and after;
+ * calls that may run at the same time need one each.  Errors: as above, OOM (workspace too small). */
+lynx_status lynx_attention_backward(const lynx_attention_config* cfg, const void* q, const void* k, const void* v,
+                                    const int32_t* offsets, const void* bias_table, const void* out, const float* lse,
+                                    const void* d_out, void* d_q, void* d_k, void* d_v, void* d_bias_table,
+                                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The usual buckets: one for each distance below E = num_buckets / 2, and from there on
+ * E + floor(log(n / E) / log(max_distance / E) (num_buckets - E)), at most num_buckets - 1.  Borders are found in whole
+ * numbers.  starts_out[num_buckets] (host); a bucket that no distance falls into starts where the next one does.
+ * Errors: INVALID_ARG (null, num_buckets not in 2..64, max_distance not in E+1..4096). */
+lynx_status lynx_position_buckets(int num_buckets, int max_distance, int32_t* starts_out);
+
 /* Measurement aid, not part of the method: a device copy of `bytes` (multiple of
  * 16; both pointers device, 16-byte aligned, not overlapping) done by a fixed
  * number of workgroups (1..4096), enqueued on `hip_stream`.  It stands in for the

@@ -32,6 +32,8 @@ LYNX_NUM_ACTIVATIONS = 14
 LYNX_PROFILE_SLOTS = 40
 LYNX_STATIC_WORKSPACE_BYTES = 64 << 20
 LYNX_FLAG_FUSED_ATTENTION = 1
+LYNX_ATTENTION_MAX_HEAD_DIM, LYNX_ATTENTION_MAX_STRIDE = 128, 1 << 21
+LYNX_MAX_BUCKETS, LYNX_MAX_DISTANCE = 64, 4096
 PARAM_FIELDS = ("wqkv", "bqkv", "wo", "bo", "w1", "b1", "w2", "b2", "g1", "be1", "g2", "be2")
 
 
@@ -69,6 +71,14 @@ class lynx_partition_problem(C.Structure):
                 ("m_budget", C.c_double)]
 
 
+class lynx_attention_config(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("tokens", C.c_int32), ("sequences", C.c_int32), ("scale", C.c_float), ("num_buckets", C.c_int32),
+                ("bucket_starts", C.POINTER(C.c_int32)), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("out_stride", C.c_int64), ("dq_stride", C.c_int64), ("dk_stride", C.c_int64),
+                ("dv_stride", C.c_int64)]
+
+
 class LynxError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -76,6 +86,7 @@ class LynxError(RuntimeError):
 
 
 _cfg_p = C.POINTER(lynx_layer_config)
+_attn_p = C.POINTER(lynx_attention_config)
 _proto = {
     "lynx_activation_bytes": (C.c_size_t, [_cfg_p, C.c_int]),
     "lynx_workspace_bytes": (C.c_size_t, [_cfg_p, C.c_uint32]),
@@ -104,6 +115,10 @@ _proto = {
     "lynx_profile_slot_name": (C.c_char_p, [C.c_int]),
     "lynx_status_string": (C.c_char_p, [C.c_int]),
     "lynx_comm_standin": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]),
+    "lynx_attention_forward": (C.c_int, [_attn_p] + [C.c_void_p] * 8),
+    "lynx_attention_backward_bytes": (C.c_size_t, [_attn_p]),
+    "lynx_attention_backward": (C.c_int, [_attn_p] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p]),
+    "lynx_position_buckets": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_int32)]),
     "lynx_policy_solve": (C.c_int, [C.POINTER(lynx_policy_problem), C.POINTER(lynx_policy)]),
     "lynx_partition_solve": (C.c_int, [C.POINTER(lynx_partition_problem), C.POINTER(C.c_int32),
                                        C.POINTER(C.c_double), C.POINTER(lynx_policy)]),
@@ -272,6 +287,29 @@ def lynx_profile_slot_name(slot: int) -> str:
 def lynx_comm_standin(dst, src, nbytes: int, workgroups: int, stream=None) -> None:
     _check(_lib.lynx_comm_standin(_addr(dst), _addr(src), nbytes, workgroups, _stream(stream)),
            "lynx_comm_standin")
+
+
+def lynx_attention_forward(cfg, q, k, v, offsets, bias_table, out, lse, stream=None) -> None:
+    _check(_lib.lynx_attention_forward(C.byref(cfg), _addr(q), _addr(k), _addr(v), _addr(offsets), _addr(bias_table), _addr(out),
+                                       _addr(lse), _stream(stream)), "lynx_attention_forward")
+
+
+def lynx_attention_backward_bytes(cfg) -> int:
+    return _lib.lynx_attention_backward_bytes(C.byref(cfg))
+
+
+def lynx_attention_backward(cfg, q, k, v, offsets, bias_table, out, lse, d_out, d_q, d_k, d_v, d_bias_table, workspace,
+                            workspace_bytes: int, stream=None) -> None:
+    _check(_lib.lynx_attention_backward(C.byref(cfg), _addr(q), _addr(k), _addr(v), _addr(offsets), _addr(bias_table), _addr(out),
+                                        _addr(lse), _addr(d_out), _addr(d_q), _addr(d_k), _addr(d_v), _addr(d_bias_table),
+                                        _addr(workspace), workspace_bytes, _stream(stream)), "lynx_attention_backward")
+
+
+def lynx_position_buckets(num_buckets: int, max_distance: int):
+    """The first distance of each bucket, as a host array for lynx_attention_config.bucket_starts."""
+    starts = (C.c_int32 * max(num_buckets, 1))()
+    _check(_lib.lynx_position_buckets(num_buckets, max_distance, starts), "lynx_position_buckets")
+    return starts
 
 
 def _mask_of(indices) -> int:

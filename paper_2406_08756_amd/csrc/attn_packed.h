@@ -1,0 +1,291 @@
+// Building blocks of the attention kernels over packed sequences (attn_packed_fwd.hip, attn_packed_bwd.hip).
+//
+// A row is a (token, query head) pair.  The 2^pack query heads of a group that stand next to each other and read the same
+// key head share a tile: row r of a sequence is token r >> pack, head r & (2^pack - 1), so that short sequences fill tiles
+// and a tile of K and V serves them all.  A sequence of n tokens has n << pack rows and n keys; row r sees the keys up to
+// its own token.
+//
+// All products are 32 x 32 blocks of the matrix instructions, D[m][n] += sum_k A[m][k] B[k][n].  Lane l holds A's row and
+// B's column l % 32, and of D's column l % 32 the rows acc_row(i, l / 32).  Formed as D = S^T (keys down, rows across), a
+// lane has the scores of one row: its maximum and sum are sums in a lane and one exchange with the other half.  The order
+// in which k is dealt to lanes and registers is free as long as A and B agree, and it is chosen so that the registers of D
+// are, rounded, the B operand of the next product, O^T += V^T P^T: no probability moves between lanes.
+#pragma once
+#include "kernels.h"
+#include "mfma_common.h"
+
+namespace lynx {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_inff();
+typedef float floatx4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ constexpr int acc_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, kWave); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < kInf; }
+
+constexpr int kRowsLog = 7;  // a workgroup has 128 rows or keys, a wavefront 32 of them
+
+// ---- which tile of which sequence ------------------------------------------
+struct SeqTile {
+  int start, len, tile;
+};
+__device__ __forceinline__ int2 sequence_span(const PackedAttn& g, int s) {
+  // (whatever the offsets hold, no row outside the tensors is named)
+  const int a = min(max(g.offsets[s], 0), g.tokens);
+  return make_int2(a, min(max(g.offsets[s + 1], a), g.tokens) - a);
+}
+// Tile number `slot`; with LAST_FIRST counted from the last, so that the tiles at the end of a long sequence, whose rows see
+// the most keys, start first (of key tiles, the first ones are seen by the most rows).
+// Every wavefront looks for itself; each lane sums the tiles of its share of the sequences, a prefix sum finds the share,
+// and the search goes on within it.  False if there are not that many tiles.
+template <bool LAST_FIRST>
+__device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int rows_log, int pack, SeqTile* out) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int first = 0, count = g.sequences, target = slot;
+  bool top = true;
+  while (true) {
+    const int per = (count + kWave - 1) / kWave;
+    int sum = 0;
+    for (int i = 0; i < per; ++i) {
+      const int s = lane * per + i;
+      if (s < count) sum += ((sequence_span(g, first + s).y << pack) + (1 << rows_log) - 1) >> rows_log;
+    }
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int v = __shfl_up(upto, o, kWave);
+      if (lane >= o) upto += v;
+    }
+    if (top) {
+      const int total = __builtin_amdgcn_readlane(upto, kWave - 1);
+      if (slot >= total) return false;
+      if (LAST_FIRST) target = total - 1 - slot;
+      top = false;
+    }
+    const int at = __builtin_ctzll(__ballot(upto > target));
+    target -= __builtin_amdgcn_readlane(upto - sum, at);
+    first += at * per;
+    count = min(per, count - at * per);
+    if (per == 1) break;
+  }
+  const int2 span = sequence_span(g, first);
+  out->start = __builtin_amdgcn_readfirstlane(span.x);
+  out->len = __builtin_amdgcn_readfirstlane(span.y);
+  out->tile = __builtin_amdgcn_readfirstlane(target);
+  return true;
+}
+
+// ---- operands ---------------------------------------------------------------
+template <typename T> struct Operand;
+template <> struct Operand<bf16_t> {
+  typedef bf16x8_t Frag;
+  static constexpr int kGroup = 16;  // rows of a column fragment pair
+  __device__ static __forceinline__ void mma(floatx16_t& acc, Frag a, Frag b) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+  }
+  // registers kGroup / 2 c .. of an accumulator block as a B operand (one rounding to the storage type: the matrix
+  // instructions take nothing wider, and the error averages out over the sum)
+  __device__ static __forceinline__ Frag from_acc(const floatx16_t& v, int c) {
+    uintx4_t w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[8 * c + 2 * j], v[8 * c + 2 * j + 1]);
+    return __builtin_bit_cast(Frag, w);
+  }
+  __device__ static __forceinline__ Frag from_raw(uintx4_t w) { return __builtin_bit_cast(Frag, w); }
+  __device__ static __forceinline__ float dot(Frag a, Frag b) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = __builtin_fmaf(static_cast<float>(a[j]), static_cast<float>(b[j]), s);
+    return s;
+  }
+};
+template <> struct Operand<float> {
+  typedef floatx4_t Frag;
+  static constexpr int kGroup = 8;
+  __device__ static __forceinline__ void mma(floatx16_t& acc, Frag a, Frag b) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], acc, 0, 0, 0);
+  }
+  __device__ static __forceinline__ Frag from_acc(const floatx16_t& v, int c) {
+    return Frag{v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
+  }
+  __device__ static __forceinline__ Frag from_raw(uintx4_t w) { return __builtin_bit_cast(Frag, w); }
+  __device__ static __forceinline__ float dot(Frag a, Frag b) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = __builtin_fmaf(a[j], b[j], s);
+    return s;
+  }
+};
+
+// 16 bytes with every infinity and NaN replaced by zero.
+__device__ __forceinline__ uintx4_t without_nonfinite(uintx4_t w, const bf16_t*) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if ((w[j] & 0x7F80u) == 0x7F80u) w[j] &= 0xFFFF0000u;
+    if ((w[j] & 0x7F800000u) == 0x7F800000u) w[j] &= 0xFFFFu;
+  }
+  return w;
+}
+__device__ __forceinline__ uintx4_t without_nonfinite(uintx4_t w, const float*) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if ((w[j] & 0x7F800000u) == 0x7F800000u) w[j] = 0;
+  return w;
+}
+
+// A tile in LDS: rows of DP elements, whose 16-byte chunks are permuted within the row so that both reads below meet all
+// 64 banks: 16 lanes of a row fragment read one chunk of 16 consecutive rows, and a transposing read takes 32 bytes of
+// each of four consecutive rows per 16 lanes (fp32: whole rows r and r + 4).
+template <typename T, int DP> struct Tile {
+  static constexpr int kChunk = 16 / static_cast<int>(sizeof(T));
+  static constexpr int kChunks = DP / kChunk;
+  static constexpr int kSteps = DP / (2 * kChunk);       // row fragments of a row
+  static constexpr int kGroups = 32 / Operand<T>::kGroup;  // column fragments of 32 rows
+  typedef typename Operand<T>::Frag Frag;
+
+  __device__ static __forceinline__ int swizzle(int row) {
+    if constexpr (sizeof(T) == 4) return (((row >> 2) & 1) << 3) | (((row >> 3) & 1) << 2) | (row & 3);
+    else if constexpr (kChunks >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+  }
+  __device__ static __forceinline__ int at(int row, int chunk) { return row * DP + (chunk ^ swizzle(row)) * kChunk; }
+  // row r0 + lane % 32, elements 2 kChunk step + kChunk (lane / 32) ..
+  __device__ static __forceinline__ Frag row_frag(const T* tile, int r0, int step, int lane) {
+    return *reinterpret_cast<const Frag*>(tile + at(r0 + (lane & 31), 2 * step + (lane >> 5)));
+  }
+  // column c0 + lane % 32 of the rows r0 + acc_row(.., lane / 32) that registers from_acc(.., c) hold
+  __device__ static __forceinline__ Frag col_frag(const T* tile, int r0, int c, int c0, int lane) {
+    if constexpr (sizeof(T) == 4) {
+      const int col = c0 + (lane & 31), row = r0 + 8 * c + 4 * (lane >> 5);
+      Frag f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = tile[at(row + j, col / kChunk) + col % kChunk];
+      return f;
+    } else {
+      // 16 lanes: lane i points at row i / 4, columns 4 (i % 4).., and receives column i of the four rows
+      const int b = lane >> 4, i = lane & 15;
+      const int row = r0 + 16 * c + 4 * (b >> 1) + (i >> 2), col = c0 + 16 * (b & 1) + 4 * (i & 3);
+      typedef __attribute__((address_space(3))) short4_t* lds_short4;
+      const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(tile + at(row, col / kChunk) + col % kChunk));
+      const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(tile + at(row + 8, col / kChunk) + col % kChunk));
+      const short8_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      return __builtin_bit_cast(Frag, v);
+    }
+  }
+};
+
+// Byte offset that every row buffer reads as zero.
+constexpr uint32_t kOutside = 0x80000000u;
+
+// ROWS rows on their way from memory to a tile: requested into registers, stored when the tile is free.
+template <typename T, int DP, int ROWS, int THREADS> struct Stage {
+  typedef Tile<T, DP> L;
+  static constexpr int kLoads = ROWS * L::kChunks / THREADS;
+  static_assert(ROWS * L::kChunks % THREADS == 0, "a tile splits over the threads");
+  uintx4_t v[kLoads];
+  // keys: rows first.. of `base` (row 0's first element), `rows` of which exist
+  __device__ __forceinline__ void load_keys(const T* base, long long stride, int first, int rows, int d) {
+    const int left = min(rows - first, ROWS);
+    const RowBuffer b = row_buffer(base + first * stride, left > 0 ? static_cast<uint32_t>((left - 1) * stride + d) * static_cast<uint32_t>(sizeof(T)) : 0u);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int e = threadIdx.x + THREADS * j, row = e / L::kChunks, col = e % L::kChunks * L::kChunk;
+      const uint32_t off = (static_cast<uint32_t>(row) * static_cast<uint32_t>(stride) + col) * static_cast<uint32_t>(sizeof(T));
+      v[j] = row_buffer_load(b, col < d ? off : kOutside);
+    }
+  }
+  // the same of rows that are (token, head) pairs; `first` is a whole token's
+  __device__ __forceinline__ void load_rows(const T* base, long long stride, int first, int tokens, int d, int pack) {
+    const int token = first >> pack, left = min(tokens - token, max(ROWS >> pack, 1)), heads = 1 << pack;
+    const RowBuffer b = row_buffer(base + token * stride, left > 0 ? static_cast<uint32_t>((left - 1) * stride + heads * d) * static_cast<uint32_t>(sizeof(T)) : 0u);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int e = threadIdx.x + THREADS * j, row = e / L::kChunks, col = e % L::kChunks * L::kChunk;
+      const uint32_t off = (static_cast<uint32_t>(row >> pack) * static_cast<uint32_t>(stride) + (row & (heads - 1)) * d + col) * static_cast<uint32_t>(sizeof(T));
+      v[j] = row_buffer_load(b, col < d ? off : kOutside);
+    }
+  }
+  template <bool CLEAN>
+  __device__ __forceinline__ void store(T* tile) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int e = threadIdx.x + THREADS * j;
+      uintx4_t w = v[j];
+      if (CLEAN) w = without_nonfinite(w, static_cast<const T*>(nullptr));
+      *reinterpret_cast<uintx4_t*>(tile + L::at(e / L::kChunks, e % L::kChunks)) = w;
+    }
+  }
+};
+
+// A wavefront's 32 rows as row fragments in registers, straight from memory.
+template <typename T, int DP>
+__device__ __forceinline__ void load_row_frags(const RowBuffer& b, uint32_t row_offset, int d, int lane, typename Operand<T>::Frag (&f)[Tile<T, DP>::kSteps]) {
+  typedef Tile<T, DP> L;
+#pragma unroll
+  for (int s = 0; s < L::kSteps; ++s) {
+    const int col = (2 * s + (lane >> 5)) * L::kChunk;
+    f[s] = Operand<T>::from_raw(row_buffer_load(b, col < d ? row_offset + col * static_cast<uint32_t>(sizeof(T)) : kOutside));
+  }
+}
+
+__device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, float d) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+}
+__device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
+
+// ---- position bias -----------------------------------------------------------
+// Bias by distance, times log2 e: `far` distances, and kPad more on both sides so that the reads of a 32-row strip against
+// 64 keys that holds one near or masked pair need no limits.
+constexpr int kPad = 96;
+__host__ __device__ __forceinline__ int table_stride(const PackedAttn& g) { return g.far + 2 * kPad; }
+__host__ __device__ __forceinline__ int table_floats(const PackedAttn& g) { return table_stride(g) << g.pack; }
+__device__ __forceinline__ int bucket_of(const PackedAttn& g, int distance) {
+  int b = 0;
+  for (int i = 1; i < g.buckets; ++i) b = distance >= g.starts[i] ? i : b;
+  return b;
+}
+template <typename T, int THREADS>
+__device__ __forceinline__ void fill_bias(const PackedAttn& g, int head0, float* by_distance) {
+  const int n = table_stride(g);
+  for (int x = threadIdx.x; x < n; x += THREADS) {
+    const int distance = x - kPad, b = bucket_of(g, distance);
+    for (int h = 0; h < (1 << g.pack); ++h)
+      by_distance[h * n + x] = load1(static_cast<const T*>(g.table) + static_cast<long long>(b) * g.heads + head0 + h) * kLog2e;
+  }
+}
+
+// ---- rows and keys that meet infinities or NaN ---------------------------------
+// A masked pair has probability 0, but 0 times infinity is NaN, and a matrix instruction multiplies every pair of its block.
+// Results that come out infinite or NaN are therefore looked at again: the tile is done once more with such elements as
+// zeros, which gives the rows that see none of them the bits that they have without them, and each row that does see some
+// is summed pair by pair, over the pairs it sees.  Nothing of this runs where all results are finite.
+template <typename T>
+__device__ __forceinline__ float row_dot(const T* x, const T* y, int d) {
+  float s = 0.f;
+  for (int c = 0; c < d; c += 8) {
+    float a[8], b[8];
+    load8(x + c, a);
+    load8(y + c, b);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = __builtin_fmaf(a[j], b[j], s);
+  }
+  return s;
+}
+template <typename T>
+__device__ __forceinline__ bool row_finite(const T* x, int d) {
+  bool ok = true;
+  for (int c = 0; c < d; c += 8) {
+    float a[8];
+    load8(x + c, a);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ok = ok && finite(a[j]);
+  }
+  return ok;
+}
+
+}  // namespace
+}  // namespace lynx

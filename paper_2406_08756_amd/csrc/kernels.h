@@ -229,4 +229,32 @@ bool gemm_pair_absorbs_gelu(int dtype, const GemmDesc& dgrad, const GemmDesc& wg
 size_t gemm_pair_colsum_bytes(int dtype, const GemmDesc& dgrad, const GemmDesc& wgrad);  // its column partials
 size_t gemm_pair_colsum_least_bytes(int dtype, const GemmDesc& dgrad, const GemmDesc& wgrad);
 
+// ---- attention over packed sequences (attn_packed_fwd.hip, attn_packed_bwd.hip) -------------------
+constexpr int kMaxBuckets = 64;
+struct PackedAttn {
+  const void *q, *k, *v;
+  const int32_t* offsets;  // [sequences + 1]
+  const void* table;       // [buckets, heads], null without a position bias
+  void* out;               // [tokens, heads d]
+  float* lse;              // [heads, tokens]
+  const void* d_out;       // backward only, from here
+  void *dq, *dk, *dv, *d_table;
+  float* delta;            // [heads, tokens]: sum over d of d_out out
+  float* partials;         // [row tiles, heads, buckets] of the table's gradient
+  long long q_stride, k_stride, v_stride, out_stride, dq_stride, dk_stride, dv_stride;  // elements between tokens
+  int sequences, tokens, heads, kv_heads, d;
+  int pack;                // log2 of the query heads whose rows share a tile
+  float scale;
+  int buckets, far;        // far: the distance from which on the last bucket holds, at least 1
+  int starts[kMaxBuckets];
+};
+hipError_t attn_packed_fwd(int dtype, const PackedAttn& g, hipStream_t st);
+hipError_t attn_packed_bwd(int dtype, const PackedAttn& g, hipStream_t st);
+// Sets `pack` from the heads and the position bias.
+void attn_packed_choose_pack(PackedAttn* g);
+// Row tiles that a launch has room for: `partials` holds [row slots, heads, buckets].
+size_t attn_packed_row_slots(const PackedAttn& g);
+// Whether its launches have few enough workgroups.
+bool attn_packed_fits(const PackedAttn& g);
+
 }  // namespace lynx
