@@ -400,13 +400,13 @@ lynx_status lynx_policy_layer_problem(const lynx_layer_config* cfg, lynx_policy_
  * positions from bucket_starts[num_buckets - 1] on are in the last bucket.
  *
  * Constraints (else LYNX_ERR_SHAPE): heads a multiple of kv_heads; head_dim a multiple
- * of 8 up to 128; tokens <= 2^24; sequences <= 2^20; num_buckets <= 64, starts <= 4096;
+ * of 8 up to 128; tokens <= 2^24; sequences <= 2^20; num_buckets <= 64, starts <= 2048;
  * strides multiples of 8, at least their row, at most 2^21.  0 < scale < infinity,
  * bucket_starts from 0 on and not decreasing (else LYNX_ERR_INVALID_ARG). */
 #define LYNX_ATTENTION_MAX_HEAD_DIM 128
 #define LYNX_ATTENTION_MAX_STRIDE (1 << 21)
 #define LYNX_MAX_BUCKETS 64
-#define LYNX_MAX_DISTANCE 4096
+#define LYNX_MAX_DISTANCE 2048
 typedef struct {
   int32_t dtype;       /* lynx_dtype: storage type of every tensor but lse */
   int32_t heads;       /* query heads */
@@ -439,7 +439,7 @@ lynx_status lynx_attention_backward(const lynx_attention_config* cfg, const void
 /* The usual buckets: one for each distance below E = num_buckets / 2, and from there on
  * E + floor(log(n / E) / log(max_distance / E) (num_buckets - E)), at most num_buckets - 1.  Borders are found in whole
  * numbers.  starts_out[num_buckets] (host); a bucket that no distance falls into starts where the next one does.
- * Errors: INVALID_ARG (null, num_buckets not in 2..64, max_distance not in E+1..4096). */
+ * Errors: INVALID_ARG (null, num_buckets not in 2..64, max_distance not in E+1..2048). */
 lynx_status lynx_position_buckets(int num_buckets, int max_distance, int32_t* starts_out);
 
 /* Measurement aid, not part of the method: a device copy of `bytes` (multiple of

@@ -33,7 +33,7 @@ LYNX_PROFILE_SLOTS = 40
 LYNX_STATIC_WORKSPACE_BYTES = 64 << 20
 LYNX_FLAG_FUSED_ATTENTION = 1
 LYNX_ATTENTION_MAX_HEAD_DIM, LYNX_ATTENTION_MAX_STRIDE = 128, 1 << 21
-LYNX_MAX_BUCKETS, LYNX_MAX_DISTANCE = 64, 4096
+LYNX_MAX_BUCKETS, LYNX_MAX_DISTANCE = 64, 2048
 PARAM_FIELDS = ("wqkv", "bqkv", "wo", "bo", "w1", "b1", "w2", "b2", "g1", "be1", "g2", "be2")
 
 

@@ -11,6 +11,8 @@
 // in which k is dealt to lanes and registers is free as long as A and B agree, and it is chosen so that the registers of D
 // are, rounded, the B operand of the next product, O^T += V^T P^T: no probability moves between lanes.
 #pragma once
+#include <mutex>
+
 #include "kernels.h"
 #include "mfma_common.h"
 
@@ -22,11 +24,33 @@ constexpr float kInf = __builtin_inff();
 typedef float floatx4_t __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ constexpr int acc_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, kWave); }
+// A value of this lane's and the one of the other half's lane, in the order of the halves.
+__device__ __forceinline__ float2 of_both_halves(float v) {
+  const uint32_t w = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+  const float2 b = of_both_halves(v);
+  return b.x + b.y;
+}
+__device__ __forceinline__ float max_of_halves(float v) {
+  const float2 b = of_both_halves(v);
+  return fmaxf(b.x, b.y);
+}
+// What is requested above is requested before anything below is done.
+__device__ __forceinline__ void requested() { __builtin_amdgcn_sched_barrier(0); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < kInf; }
 
-constexpr int kRowsLog = 7;  // a workgroup has 128 rows or keys, a wavefront 32 of them
+// A wavefront has 32 rows (or keys).  A workgroup has 128, whose wavefronts share the tiles that they go through; or, where
+// there are too few of those to fill the card (SPLIT), 32, whose wavefronts deal the 32-key tiles among themselves, each on
+// its own without a barrier, and join their parts at the end.
+constexpr int rows_log(bool split) { return split ? 5 : 7; }
+__device__ __forceinline__ void wave_fence() {  // the wavefront's LDS accesses stay in program order
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 // ---- which tile of which sequence ------------------------------------------
 struct SeqTile {
@@ -42,7 +66,7 @@ __device__ __forceinline__ int2 sequence_span(const PackedAttn& g, int s) {
 // Every wavefront looks for itself; each lane sums the tiles of its share of the sequences, a prefix sum finds the share,
 // and the search goes on within it.  False if there are not that many tiles.
 template <bool LAST_FIRST>
-__device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int rows_log, int pack, SeqTile* out) {
+__device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int tile_log, int pack, SeqTile* out) {
   const int lane = threadIdx.x & (kWave - 1);
   int first = 0, count = g.sequences, target = slot;
   bool top = true;
@@ -51,7 +75,7 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int row
     int sum = 0;
     for (int i = 0; i < per; ++i) {
       const int s = lane * per + i;
-      if (s < count) sum += ((sequence_span(g, first + s).y << pack) + (1 << rows_log) - 1) >> rows_log;
+      if (s < count) sum += ((sequence_span(g, first + s).y << pack) + (1 << tile_log) - 1) >> tile_log;
     }
     int upto = sum;
 #pragma unroll
@@ -153,28 +177,40 @@ template <typename T, int DP> struct Tile {
     else return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
   }
   __device__ static __forceinline__ int at(int row, int chunk) { return row * DP + (chunk ^ swizzle(row)) * kChunk; }
-  // row r0 + lane % 32, elements 2 kChunk step + kChunk (lane / 32) ..
-  __device__ static __forceinline__ Frag row_frag(const T* tile, int r0, int step, int lane) {
-    return *reinterpret_cast<const Frag*>(tile + at(r0 + (lane & 31), 2 * step + (lane >> 5)));
+  // Fragments are read at a lane's own offset (bytes, of the first fragment), whose swizzled bits the step, column block and
+  // row group change by exclusive ors alone: one register serves all of them.  r0 is a multiple of 32.
+  // Row r0 + lane % 32, elements 2 kChunk step + kChunk (lane / 32) ..:
+  __device__ static __forceinline__ uint32_t row_base(int lane) { return at(lane & 31, lane >> 5) * static_cast<int>(sizeof(T)); }
+  __device__ static __forceinline__ Frag row_frag(const T* tile, uint32_t base, int r0, int step) {
+    return *reinterpret_cast<const Frag*>(bytes(tile, base ^ (step << 5)) + r0 * kRowBytes);
   }
-  // column c0 + lane % 32 of the rows r0 + acc_row(.., lane / 32) that registers from_acc(.., c) hold
-  __device__ static __forceinline__ Frag col_frag(const T* tile, int r0, int c, int c0, int lane) {
+  // Column 32 e + lane % 32 of the rows r0 + acc_row(.., lane / 32) that registers from_acc(.., c) hold.  bf16, 16 lanes: lane i
+  // points at row i / 4, columns 4 (i % 4).., and receives column i of the four rows.
+  __device__ static __forceinline__ uint32_t col_base(int lane) {
+    const int b = lane >> 4, i = lane & 15;
+    const int row = sizeof(T) == 4 ? 4 * (lane >> 5) : 4 * (b >> 1) + (i >> 2), col = sizeof(T) == 4 ? lane & 31 : 16 * (b & 1) + 4 * (i & 3);
+    return (at(row, col / kChunk) + col % kChunk) * static_cast<int>(sizeof(T));
+  }
+  __device__ static __forceinline__ Frag col_frag(const T* tile, uint32_t base, int r0, int c, int e) {
     if constexpr (sizeof(T) == 4) {
-      const int col = c0 + (lane & 31), row = r0 + 8 * c + 4 * (lane >> 5);
       Frag f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] = tile[at(row + j, col / kChunk) + col % kChunk];
+      for (int j = 0; j < 4; ++j)
+        f[j] = *reinterpret_cast<const float*>(bytes(tile, base ^ (e << 7) ^ ((c & 1) << 6) ^ (j << 4)) + (r0 + 8 * c + j) * kRowBytes);
       return f;
     } else {
-      // 16 lanes: lane i points at row i / 4, columns 4 (i % 4).., and receives column i of the four rows
-      const int b = lane >> 4, i = lane & 15;
-      const int row = r0 + 16 * c + 4 * (b >> 1) + (i >> 2), col = c0 + 16 * (b & 1) + 4 * (i & 3);
       typedef __attribute__((address_space(3))) short4_t* lds_short4;
-      const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(tile + at(row, col / kChunk) + col % kChunk));
-      const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(tile + at(row + 8, col / kChunk) + col % kChunk));
+      const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(bytes(tile, base ^ (e << 6)) + (r0 + 16 * c) * kRowBytes));
+      const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(bytes(tile, base ^ (e << 6) ^ 32) + (r0 + 16 * c + 8) * kRowBytes));
       const short8_t v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       return __builtin_bit_cast(Frag, v);
     }
+  }
+
+ private:
+  static constexpr int kRowBytes = DP * static_cast<int>(sizeof(T));
+  __device__ static __forceinline__ const unsigned char* bytes(const T* tile, uint32_t offset) {
+    return reinterpret_cast<const unsigned char*>(tile) + offset;
   }
 };
 
@@ -182,38 +218,39 @@ template <typename T, int DP> struct Tile {
 constexpr uint32_t kOutside = 0x80000000u;
 
 // ROWS rows on their way from memory to a tile: requested into registers, stored when the tile is free.
+// THREADS threads (`who` of them) do it together.
 template <typename T, int DP, int ROWS, int THREADS> struct Stage {
   typedef Tile<T, DP> L;
   static constexpr int kLoads = ROWS * L::kChunks / THREADS;
   static_assert(ROWS * L::kChunks % THREADS == 0, "a tile splits over the threads");
   uintx4_t v[kLoads];
   // keys: rows first.. of `base` (row 0's first element), `rows` of which exist
-  __device__ __forceinline__ void load_keys(const T* base, long long stride, int first, int rows, int d) {
+  __device__ __forceinline__ void load_keys(const T* base, long long stride, int first, int rows, int d, int who) {
     const int left = min(rows - first, ROWS);
     const RowBuffer b = row_buffer(base + first * stride, left > 0 ? static_cast<uint32_t>((left - 1) * stride + d) * static_cast<uint32_t>(sizeof(T)) : 0u);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int e = threadIdx.x + THREADS * j, row = e / L::kChunks, col = e % L::kChunks * L::kChunk;
+      const int e = who + THREADS * j, row = e / L::kChunks, col = e % L::kChunks * L::kChunk;
       const uint32_t off = (static_cast<uint32_t>(row) * static_cast<uint32_t>(stride) + col) * static_cast<uint32_t>(sizeof(T));
       v[j] = row_buffer_load(b, col < d ? off : kOutside);
     }
   }
   // the same of rows that are (token, head) pairs; `first` is a whole token's
-  __device__ __forceinline__ void load_rows(const T* base, long long stride, int first, int tokens, int d, int pack) {
+  __device__ __forceinline__ void load_rows(const T* base, long long stride, int first, int tokens, int d, int pack, int who) {
     const int token = first >> pack, left = min(tokens - token, max(ROWS >> pack, 1)), heads = 1 << pack;
     const RowBuffer b = row_buffer(base + token * stride, left > 0 ? static_cast<uint32_t>((left - 1) * stride + heads * d) * static_cast<uint32_t>(sizeof(T)) : 0u);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int e = threadIdx.x + THREADS * j, row = e / L::kChunks, col = e % L::kChunks * L::kChunk;
+      const int e = who + THREADS * j, row = e / L::kChunks, col = e % L::kChunks * L::kChunk;
       const uint32_t off = (static_cast<uint32_t>(row >> pack) * static_cast<uint32_t>(stride) + (row & (heads - 1)) * d + col) * static_cast<uint32_t>(sizeof(T));
       v[j] = row_buffer_load(b, col < d ? off : kOutside);
     }
   }
   template <bool CLEAN>
-  __device__ __forceinline__ void store(T* tile) {
+  __device__ __forceinline__ void store(T* tile, int who) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int e = threadIdx.x + THREADS * j;
+      const int e = who + THREADS * j;
       uintx4_t w = v[j];
       if (CLEAN) w = without_nonfinite(w, static_cast<const T*>(nullptr));
       *reinterpret_cast<uintx4_t*>(tile + L::at(e / L::kChunks, e % L::kChunks)) = w;
@@ -244,8 +281,10 @@ constexpr int kPad = 96;
 __host__ __device__ __forceinline__ int table_stride(const PackedAttn& g) { return g.far + 2 * kPad; }
 __host__ __device__ __forceinline__ int table_floats(const PackedAttn& g) { return table_stride(g) << g.pack; }
 __device__ __forceinline__ int bucket_of(const PackedAttn& g, int distance) {
+  // (all kMaxBuckets starts, those behind the last bucket at the largest number: a loop to the last would wait for each)
   int b = 0;
-  for (int i = 1; i < g.buckets; ++i) b = distance >= g.starts[i] ? i : b;
+#pragma unroll
+  for (int i = 1; i < kMaxBuckets; ++i) b += distance >= g.starts[i] ? 1 : 0;
   return b;
 }
 template <typename T, int THREADS>
@@ -256,6 +295,60 @@ __device__ __forceinline__ void fill_bias(const PackedAttn& g, int head0, float*
     for (int h = 0; h < (1 << g.pack); ++h)
       by_distance[h * n + x] = load1(static_cast<const T*>(g.table) + static_cast<long long>(b) * g.heads + head0 + h) * kLog2e;
   }
+}
+
+constexpr int kMostLds = 159 << 10;  // (the barrier that joins a truth value has 1 KB of its own)
+template <auto KERNEL>
+hipError_t launch_packed(size_t groups, size_t lds, const PackedAttn& g, hipStream_t st) {
+  static std::once_flag once;
+  static hipError_t limit = hipSuccess;
+  std::call_once(once, [] { limit = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds); });
+  if (limit != hipSuccess) return limit;
+  hipLaunchKernelGGL(KERNEL, dim3(static_cast<unsigned>(groups)), dim3(kThreads), lds, st, g);
+  return hipGetLastError();
+}
+
+// ---- joining the parts of a SPLIT workgroup's wavefronts ----------------------
+// A part: [DP columns][32 rows] floats, as the accumulator blocks hold them; it takes the wavefront's two tiles' place.
+template <int DP>
+__device__ __forceinline__ void write_part(float* part, const floatx16_t (&acc)[DP / 32], float factor, int lane) {
+#pragma unroll
+  for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) part[(32 * b + acc_row(i, lane >> 5)) * 32 + (lane & 31)] = acc[b][i] * factor;
+}
+// The sum of the parts, in the order of the wavefronts: DP / 8 columns from join_column of row lane % 32.
+template <int DP> __device__ __forceinline__ int join_column(int wave, int lane) { return wave * (DP / 4) + (lane >> 5) * (DP / 8); }
+template <int DP>
+__device__ __forceinline__ void join_parts(const float* parts, size_t part_floats, int wave, int lane, float (&sum)[DP / 8]) {
+  const int at = join_column<DP>(wave, lane) * 32 + (lane & 31);
+#pragma unroll
+  for (int c = 0; c < DP / 8; ++c) {
+    sum[c] = parts[at + 32 * c];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) sum[c] += parts[w * part_floats + at + 32 * c];
+  }
+}
+template <typename T, int DP>
+__device__ __forceinline__ void store_joined(T* row, int column, int d, const float (&sum)[DP / 8], float factor) {
+#pragma unroll
+  for (int c = 0; c < DP / 8; c += 8) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = sum[c + j] * factor;
+    if (column + c < d) store8(row + column + c, v);
+  }
+}
+
+// Every wavefront's bits together, dealt out again: this one has those whose number is its own modulo the wavefronts.
+__device__ __forceinline__ uint32_t share_rows(uint32_t rows, uint32_t* all, int wave) {
+  __syncthreads();
+  all[wave] = rows;
+  __syncthreads();
+  uint32_t any = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) any |= all[w];
+  return any & (0x11111111u << wave);
 }
 
 // ---- rows and keys that meet infinities or NaN ---------------------------------

@@ -37,16 +37,17 @@ lynx_status make_args(const lynx_attention_config* c, bool backward, PackedAttn*
     if (c->bucket_starts[i] > LYNX_MAX_DISTANCE) return LYNX_ERR_SHAPE;
     g->starts[i] = c->bucket_starts[i];
   }
+  for (int i = c->num_buckets; i < lynx::kMaxBuckets; ++i) g->starts[i] = INT32_MAX;
   g->far = c->num_buckets > 0 && g->starts[c->num_buckets - 1] > 1 ? g->starts[c->num_buckets - 1] : 1;
-  lynx::attn_packed_choose_pack(g);
+  lynx::attn_packed_choose(c->dtype == LYNX_BF16 ? 1 : 0, g);
   return lynx::attn_packed_fits(*g) ? LYNX_OK : LYNX_ERR_SHAPE;
 }
 
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 size_t delta_bytes(const PackedAttn& g) { return round_up(static_cast<size_t>(g.heads) * g.tokens * sizeof(float)); }
-size_t partials_bytes(const PackedAttn& g) { return round_up(lynx::attn_packed_row_slots(g) * g.heads * g.buckets * sizeof(float)); }
+size_t partials_bytes(const PackedAttn& g) { return round_up(lynx::attn_packed_row_slots(g, g.split_rows) * g.heads * g.buckets * sizeof(float)); }
 
-// (a b)^.. in whole numbers, for the borders of the buckets: at most 64 factors below 2^13
+// (a b)^.. in whole numbers, for the borders of the buckets: at most 64 factors below 2^12
 struct Whole {
   static constexpr int kWords = 32;
   uint32_t w[kWords] = {1};

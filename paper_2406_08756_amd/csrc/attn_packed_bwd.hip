@@ -9,16 +9,25 @@
 namespace lynx {
 namespace {
 
-constexpr int kHistStride = kThreads + 1;  // a column of the histogram: one float per thread
+// The gradient of the position bias.  ds by distance, for each head of the tile and each wavefront apart: `far` distances and
+// what a 32 x 32 block that holds one of them reaches beyond.  A near block is laid down in LDS and a lane adds up one of its
+// diagonals, so that each sum has one owner and one order; blocks whose keys are all far are summed in a register.
+constexpr int kBlockStride = 33, kBlockPad = 32, kBlockFloats = 32 * kBlockStride + 2 * kBlockPad;
+__host__ __device__ __forceinline__ int distances(const PackedAttn& g) { return g.far + 64; }
+__host__ __device__ __forceinline__ int by_distance_floats(const PackedAttn& g) { return (distances(g) << g.pack) + kBlockFloats; }  // of a wavefront
 
-template <typename T, int DP, bool BIAS> struct Rows {
-  static constexpr int kKeys = sizeof(T) == 2 && !BIAS ? 64 : 32;
-  static constexpr size_t kLds = 4 * static_cast<size_t>(kKeys) * DP * sizeof(T);
+// Two tiles, two of each, or one of each wavefront.
+template <typename T, int DP, bool BIAS, bool SPLIT> struct Rows {
+  static constexpr int kKeys = sizeof(T) == 2 && !BIAS && !SPLIT ? 64 : 32;
+  static constexpr int kTileElems = kKeys * DP;
+  static constexpr size_t kTiles = (SPLIT ? 2 * kWaves : 4) * static_cast<size_t>(kTileElems) * sizeof(T);
+  static constexpr size_t kLds = kTiles + (SPLIT ? kWaves * sizeof(uint32_t) : 0);
 };
-template <typename T, int DP> struct Keys {
-  static constexpr int kRows = sizeof(T) == 2 ? 64 : 32;
-  static constexpr size_t kTiles = 4 * static_cast<size_t>(kRows) * DP * sizeof(T);
-  static constexpr size_t kLds = kTiles + 4 * kRows * sizeof(float);
+template <typename T, int DP, bool SPLIT> struct Keys {
+  static constexpr int kRows = sizeof(T) == 2 && !SPLIT ? 64 : 32;
+  static constexpr int kTileElems = kRows * DP;
+  static constexpr size_t kTiles = (SPLIT ? 2 * kWaves : 4) * static_cast<size_t>(kTileElems) * sizeof(T);
+  static constexpr size_t kLds = kTiles + (SPLIT ? 2 * kWaves : 4) * kRows * sizeof(float) + (SPLIT ? kWaves * sizeof(uint32_t) : 0);
 };
 
 // The statistic as the exponent's offset; a row that sees nothing but minus infinity has probabilities of zero.
@@ -54,18 +63,16 @@ __device__ void sum_row_dq(const PackedAttn& g, const T* q, const T* d_out, cons
     if (lane + kWave * c < g.d) store1(dq + lane + kWave * c, acc[c] * g.scale);
 }
 
-template <typename T, int DP, bool BIAS>
+template <typename T, int DP, bool BIAS, bool SPLIT>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void attn_packed_rows_kernel(PackedAttn g) {
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
-  typedef Rows<T, DP, BIAS> S;
-  constexpr int kKeys = S::kKeys;
+  typedef Rows<T, DP, BIAS, SPLIT> S;
+  constexpr int kKeys = S::kKeys, kTileElems = S::kTileElems, kRowsLog = rows_log(SPLIT);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   T* const lds = reinterpret_cast<T*>(smem_raw);
-  constexpr int kTileElems = kKeys * DP;
   float* const bias = reinterpret_cast<float*>(smem_raw + S::kLds);
-  float* const hist = bias + (BIAS ? table_floats(g) : 0);
-  unsigned char* const bucket = reinterpret_cast<unsigned char*>(hist + (BIAS ? g.buckets * kHistStride : 0));  // by distance
+  float* const sums = bias + (BIAS ? table_floats(g) : 0);  // of the table's gradient: by_distance_floats per wavefront
 
   const int subs = g.heads >> g.pack, slot = static_cast<int>(blockIdx.x) / subs;
   const int head0 = (static_cast<int>(blockIdx.x) % subs) << g.pack;
@@ -81,8 +88,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   }
   if (BIAS) {
     fill_bias<T, kThreads>(g, head0, bias);
-    for (int x = threadIdx.x; x < table_stride(g); x += kThreads) bucket[x] = static_cast<unsigned char>(bucket_of(g, x - kPad));
-    for (int x = threadIdx.x; x < g.buckets * kHistStride; x += kThreads) hist[x] = 0.f;
+    for (int x = threadIdx.x; x < kWaves * by_distance_floats(g); x += kThreads) sums[x] = 0.f;
   }
 
   const int kv = head0 / (g.heads / g.kv_heads);
@@ -93,7 +99,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   const T* const d_out = static_cast<const T*>(g.d_out) + w.start * g.out_stride + static_cast<long long>(head0) * g.d;
   T* const dq = static_cast<T*>(g.dq) + w.start * g.dq_stride + static_cast<long long>(head0) * g.d;
 
-  const int row0 = (w.tile << kRowsLog) + 32 * wave;
+  const int row0 = (w.tile << kRowsLog) + (SPLIT ? 0 : 32 * wave);
   const int row = row0 + (lane & 31), tok = row >> g.pack, hp = row & (heads - 1);
   const int first_tok = row0 >> g.pack, last_tok = first_tok < w.len ? min((row0 + 31) >> g.pack, w.len - 1) : -1;
   const bool there = tok < w.len;
@@ -113,106 +119,156 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
     load_row_frags<T, DP>(buffer(d_out, g.out_stride), at(g.out_stride), g.d, lane, gf);
 #pragma unroll
     for (int s = 0; s < L::kSteps; ++s) delta += Op::dot(qf[s], gf[s]);
-    delta += other_half(delta);
+    delta = sum_of_halves(delta);
     load_row_frags<T, DP>(buffer(q, g.q_stride), at(g.q_stride), g.d, lane, qf);
     if (there) {
       const long long stat = static_cast<long long>(head0 + hp) * g.tokens + w.start + tok;
       lse2 = offset2(g.lse[stat]);
-      if (half == 0) g.delta[stat] = delta;
+      if (half == 0 && (!SPLIT || wave == 0)) g.delta[stat] = delta;
     }
   }
-  const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);
-  const int tiles = (end_tok + kKeys - 1) / kKeys;
   const float* const my_bias = BIAS ? bias + hp * table_stride(g) + kPad : nullptr;
+  float* const my_sums = BIAS ? sums + wave * by_distance_floats(g) : nullptr;
   float far_sum = 0.f;
+  if (SPLIT && BIAS) __syncthreads();
 
-  Stage<T, DP, kKeys, kThreads> sk, sv;
+  constexpr int kTogether = SPLIT ? kWave : kThreads;
+  const int who = SPLIT ? lane : static_cast<int>(threadIdx.x);
+  Stage<T, DP, kKeys, kTogether> sk, sv;
   floatx16_t acc[DP / 32];
+  const auto load = [&](int t) {
+    sk.load_keys(k, g.k_stride, t * kKeys, w.len, g.d, who);
+    sv.load_keys(v, g.v_stride, t * kKeys, w.len, g.d, who);
+  };
+  const auto store = [&](T* tile, bool clean) {
+    if (clean) sk.template store<true>(tile, who);
+    else sk.template store<false>(tile, who);
+    sv.template store<false>(tile + kTileElems, who);
+  };
+  const uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
+  // 32 keys from key0 on, rows b0.. of kt and vt
+  const auto attend = [&](const T* kt, const T* vt, int b0, int key0, bool clean) {
+    floatx16_t s{}, dp{};
+#pragma unroll
+    for (int c = 0; c < L::kSteps; ++c) Op::mma(s, L::row_frag(kt, row_base, b0, c), qf[c]);
+#pragma unroll
+    for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, L::row_frag(vt, row_base, b0, c), gf[c]);
+    const int apart = tok - key0 - 4 * half;
+    const bool near = BIAS && first_tok - (key0 + 31) < g.far, edge = key0 + 31 > first_tok;
+    const float offset = BIAS && !near ? lse2 - my_bias[g.far] : lse2;
+    if (BIAS && near) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale2, my_bias[apart - acc_row(i, 0)] - lse2);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale2, -offset);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i]) * (dp[i] - delta);
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (apart < acc_row(i, 0)) s[i] = 0.f;
+    }
+    if (!there) s = floatx16_t{};
+    if (BIAS && !clean) {
+      if (near) {
+        float* const block = my_sums + (distances(g) << g.pack) + kBlockPad;
+        wave_fence();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) block[(lane & 31) * kBlockStride + acc_row(i, half)] = s[i];
+        wave_fence();
+        // lane: the diagonal token - key = lane - 31, of each head in turn
+        const int diagonal = lane - 31, distance = first_tok - key0 + diagonal, tokens = 32 >> g.pack;
+        for (int h = 0; h < heads; ++h) {
+          float sum = 0.f;
+#pragma unroll 8
+          for (int r = 0; r < tokens; ++r) {
+            const float x = block[((r << g.pack) + h) * kBlockStride + r - diagonal];
+            sum += r - diagonal >= 0 && r - diagonal < 32 ? x : 0.f;
+          }
+          if (distance >= 0 && diagonal < tokens) my_sums[h * distances(g) + distance] += sum;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) far_sum += s[i];
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < L::kGroups; ++c) {
+      const typename Op::Frag ds = Op::from_acc(s, c);
+#pragma unroll
+      for (int e = 0; e < DP / 32; ++e) Op::mma(acc[e], L::col_frag(kt, col_base, b0, c, e), ds);
+    }
+  };
+
   bool spoilt = false;
+  float joined[DP / 8];  // SPLIT: this lane's columns of its row
   for (bool clean = false;; clean = true) {
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) acc[b] = floatx16_t{};
-    sk.load_keys(k, g.k_stride, 0, w.len, g.d);
-    sv.load_keys(v, g.v_stride, 0, w.len, g.d);
-    for (int t = 0; t < tiles; ++t) {
-      T* const kt = lds + (t & 1) * 2 * kTileElems;
-      T* const vt = kt + kTileElems;
-      if (clean) sk.template store<true>(kt);
-      else sk.template store<false>(kt);
-      sv.template store<false>(vt);
-      __syncthreads();
-      if (t + 1 < tiles) {
-        sk.load_keys(k, g.k_stride, (t + 1) * kKeys, w.len, g.d);
-        sv.load_keys(v, g.v_stride, (t + 1) * kKeys, w.len, g.d);
+    if constexpr (SPLIT) {
+      T* const mine = lds + wave * 2 * kTileElems;
+      const int tiles = last_tok / kKeys + 1;
+      if (wave < tiles) load(wave);
+      for (int t = wave; t < tiles; t += kWaves) {
+        wave_fence();
+        store(mine, clean);
+        wave_fence();
+        if (t + kWaves < tiles) load(t + kWaves);
+        attend(mine, mine + kTileElems, 0, t * kKeys, clean);
       }
+      __syncthreads();
+      float* const parts = reinterpret_cast<float*>(smem_raw);
+      constexpr size_t kPart = 2 * kTileElems * sizeof(T) / sizeof(float);
+      static_assert(32 * DP <= kPart, "the parts take the tiles' place");
+      write_part<DP>(parts + wave * kPart, acc, 1.f, lane);
+      __syncthreads();
+      join_parts<DP>(parts, kPart, wave, lane, joined);
+    } else {
+      const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);
+      const int tiles = (end_tok + kKeys - 1) / kKeys;
+      load(0);
+      for (int t = 0; t < tiles; ++t) {
+        T* const tile = lds + (t & 1) * 2 * kTileElems;
+        store(tile, clean);
+        __syncthreads();
+        if (t + 1 < tiles) load(t + 1);
 #pragma unroll
-      for (int b = 0; b < kKeys / 32; ++b) {
-        const int key0 = t * kKeys + 32 * b;
-        if (key0 > last_tok) continue;
-        floatx16_t s{}, dp{};
-#pragma unroll
-        for (int c = 0; c < L::kSteps; ++c) Op::mma(s, L::row_frag(kt, 32 * b, c, lane), qf[c]);
-#pragma unroll
-        for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, L::row_frag(vt, 32 * b, c, lane), gf[c]);
-        const int apart = tok - key0 - 4 * half;
-        const bool near = BIAS && first_tok - (key0 + 31) < g.far, edge = key0 + 31 > first_tok;
-        const float offset = BIAS && !near ? lse2 - my_bias[g.far] : lse2;
-        if (BIAS && near) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale2, my_bias[apart - acc_row(i, 0)] - lse2);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale2, -offset);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i]) * (dp[i] - delta);
-        if (edge) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (apart < acc_row(i, 0)) s[i] = 0.f;
-        }
-        if (!there) s = floatx16_t{};
-        if (BIAS && !clean) {
-          if (near) {
-            // (each thread adds to a column of its own, in program order)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              __hip_atomic_fetch_add(hist + bucket[apart - acc_row(i, 0) + kPad] * kHistStride + threadIdx.x, s[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) far_sum += s[i];
-          }
-        }
-#pragma unroll
-        for (int c = 0; c < L::kGroups; ++c) {
-          const typename Op::Frag ds = Op::from_acc(s, c);
-#pragma unroll
-          for (int e = 0; e < DP / 32; ++e) Op::mma(acc[e], L::col_frag(kt, 32 * b, c, 32 * e, lane), ds);
-        }
+        for (int b = 0; b < kKeys / 32; ++b)
+          if (t * kKeys + 32 * b <= last_tok) attend(tile, tile + kTileElems, 32 * b, t * kKeys + 32 * b, clean);
       }
     }
     if (clean) break;
     float check = 0.f;
+    if constexpr (SPLIT) {
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
+      for (int c = 0; c < DP / 8; ++c) check = __builtin_fmaf(joined[c], 0.f, check);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) check = __builtin_fmaf(acc[b][i], 0.f, check);
-    check += other_half(check);
+      for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) check = __builtin_fmaf(acc[b][i], 0.f, check);
+    }
+    check = sum_of_halves(check);
     spoilt = there && check != 0.f;
     if (!__syncthreads_or(spoilt)) break;
   }
   if (there) {
     T* const mine = dq + tok * g.dq_stride + hp * g.d;
+    if constexpr (SPLIT) store_joined<T, DP>(mine, join_column<DP>(wave, lane), g.d, joined, g.scale);
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
+    for (int b = 0; b < (SPLIT ? 0 : DP / 32); ++b)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const int col = 32 * b + acc_row(i, half);
         if (col < g.d) store4(mine + col, acc[b][i] * g.scale, acc[b][i + 1] * g.scale, acc[b][i + 2] * g.scale, acc[b][i + 3] * g.scale);
       }
   }
-  if (__any(spoilt)) __threadfence();
-  for (uint32_t rows = static_cast<uint32_t>(__ballot(spoilt)); rows != 0; rows &= rows - 1) {
+  uint32_t spoilt_rows = static_cast<uint32_t>(__ballot(spoilt));
+  if constexpr (SPLIT) spoilt_rows = share_rows(spoilt_rows, reinterpret_cast<uint32_t*>(smem_raw + S::kTiles), wave);
+  if (spoilt_rows != 0) __threadfence();
+  for (uint32_t rows = spoilt_rows; rows != 0; rows &= rows - 1) {
     const int r = __builtin_ctz(rows), t = (row0 + r) >> g.pack, h = (row0 + r) & (heads - 1);
     sum_row_dq(g, q + t * g.q_stride + h * g.d, d_out + t * g.out_stride + h * g.d, k, v, t,
                __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse2), r)),
@@ -220,13 +276,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
                dq + t * g.dq_stride + h * g.d);
   }
   if (BIAS) {
-    hist[(g.buckets - 1) * kHistStride + threadIdx.x] += far_sum;
+    // the far part goes to the first far distance; then the wavefronts' sums together, and those of a bucket's distances
+    for (int o = 32; o >= heads; o >>= 1) far_sum += __shfl_xor(far_sum, o, kWave);
+    if (lane < heads) my_sums[lane * distances(g) + g.far] += far_sum;
     __syncthreads();
-    for (int x = threadIdx.x; x < heads * g.buckets; x += kThreads) {
+    for (int x = threadIdx.x; x < heads * distances(g); x += kThreads)
+#pragma unroll
+      for (int i = 1; i < kWaves; ++i) sums[x] += sums[i * by_distance_floats(g) + x];
+    __syncthreads();
+    for (int x = threadIdx.x / 8; x < heads * g.buckets; x += kThreads / 8) {
       const int h = x / g.buckets, b = x % g.buckets;
+      const int end = b + 1 < g.buckets ? min(g.starts[b + 1], distances(g)) : distances(g);
       float sum = 0.f;
-      for (int r = h; r < kThreads; r += heads) sum += hist[b * kHistStride + r];  // (a thread's head: its number modulo the heads)
-      g.partials[(static_cast<long long>(slot) * g.heads + head0 + h) * g.buckets + b] = sum;
+      for (int at = g.starts[b] + (threadIdx.x & 7); at < end; at += 8) sum += sums[h * distances(g) + at];
+      sum = group8_sum(sum);
+      if ((threadIdx.x & 7) == 0) g.partials[(static_cast<long long>(slot) * g.heads + head0 + h) * g.buckets + b] = sum;
     }
   }
 }
@@ -275,21 +339,20 @@ __device__ void sum_key(const PackedAttn& g, const SeqTile& w, int kv, int key, 
     }
 }
 
-template <typename T, int DP, bool BIAS>
+template <typename T, int DP, bool BIAS, bool SPLIT>
 __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_kernel(PackedAttn g) {
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
-  typedef Keys<T, DP> S;
-  constexpr int kRows = S::kRows;
+  typedef Keys<T, DP, SPLIT> S;
+  constexpr int kRows = S::kRows, kTileElems = S::kTileElems, kKeysLog = rows_log(SPLIT);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   T* const lds = reinterpret_cast<T*>(smem_raw);
-  constexpr int kTileElems = kRows * DP;
-  float* const stats = reinterpret_cast<float*>(smem_raw + S::kTiles);  // offsets and deltas, two of each
-  float* const bias = stats + 4 * kRows;
+  float* const stats = reinterpret_cast<float*>(smem_raw + S::kTiles);  // offsets and deltas, like the tiles
+  float* const bias = reinterpret_cast<float*>(smem_raw + S::kLds);
 
   const int kv = static_cast<int>(blockIdx.x) % g.kv_heads;
   SeqTile w;
-  if (!find_tile</*LAST_FIRST=*/false>(g, static_cast<int>(blockIdx.x) / g.kv_heads, kRowsLog, 0, &w)) return;
+  if (!find_tile</*LAST_FIRST=*/false>(g, static_cast<int>(blockIdx.x) / g.kv_heads, kKeysLog, 0, &w)) return;
 
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -299,7 +362,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
   const T* const q = static_cast<const T*>(g.q) + w.start * g.q_stride + static_cast<long long>(kv * group) * g.d;
   const T* const d_out = static_cast<const T*>(g.d_out) + w.start * g.out_stride + static_cast<long long>(kv * group) * g.d;
   const float scale2 = g.scale * kLog2e;
-  const int tile_key0 = w.tile << kRowsLog, key0 = tile_key0 + 32 * wave, key = key0 + (lane & 31);
+  const int tile_key0 = w.tile << kKeysLog, key0 = tile_key0 + (SPLIT ? 0 : 32 * wave), key = key0 + (lane & 31);
   const bool there = key < w.len;
 
   typename Op::Frag kf[L::kSteps], vf[L::kSteps];
@@ -314,14 +377,16 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
   const int first_row = tile_key0 << g.pack, rows = w.len << g.pack;
   const int tiles = (rows - first_row + kRows - 1) / kRows, steps = tiles * subs;
 
-  Stage<T, DP, kRows, kThreads> sq, sg;
+  constexpr int kTogether = SPLIT ? kWave : kThreads;
+  const int who = SPLIT ? lane : static_cast<int>(threadIdx.x);
+  Stage<T, DP, kRows, kTogether> sq, sg;
   float next_lse = kInf, next_delta = 0.f;
   const auto load = [&](int it) {
     const int sub = it / tiles, r0 = first_row + it % tiles * kRows;
-    sq.load_rows(q + static_cast<long long>(sub << g.pack) * g.d, g.q_stride, r0, w.len, g.d, g.pack);
-    sg.load_rows(d_out + static_cast<long long>(sub << g.pack) * g.d, g.out_stride, r0, w.len, g.d, g.pack);
-    if (threadIdx.x < kRows) {
-      const int r = r0 + threadIdx.x;
+    sq.load_rows(q + static_cast<long long>(sub << g.pack) * g.d, g.q_stride, r0, w.len, g.d, g.pack, who);
+    sg.load_rows(d_out + static_cast<long long>(sub << g.pack) * g.d, g.out_stride, r0, w.len, g.d, g.pack, who);
+    if (who < kRows) {
+      const int r = r0 + who;
       next_lse = kInf;  // (rows behind the last: probabilities of zero)
       next_delta = 0.f;
       if (r < rows) {
@@ -331,92 +396,143 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
       }
     }
   };
+  const auto store = [&](T* tile, float* stat, bool clean) {
+    if (clean) {
+      sq.template store<true>(tile, who);
+      sg.template store<true>(tile + kTileElems, who);
+    } else {
+      sq.template store<false>(tile, who);
+      sg.template store<false>(tile + kTileElems, who);
+    }
+    if (who < kRows) {
+      stat[who] = next_lse;
+      stat[kRows + who] = next_delta;
+    }
+  };
 
   floatx16_t dk[DP / 32], dv[DP / 32];
+  const uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
+  // 32 rows from r0 on, rows b0.. of qt, gt and of the statistics
+  const auto attend = [&](const T* qt, const T* gt, const float* lse_t, int b0, int r0) {
+    const int first_tok = r0 >> g.pack;
+    floatx16_t s{}, dp{};
+#pragma unroll
+    for (int c = 0; c < L::kSteps; ++c) Op::mma(s, L::row_frag(qt, row_base, b0, c), kf[c]);
+#pragma unroll
+    for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, L::row_frag(gt, row_base, b0, c), vf[c]);
+    // register i: token first_tok + (i's part, the same for all lanes) + (4 half >> pack), head likewise
+    const int apart = first_tok + ((4 * half) >> g.pack) - key;
+    const int stride = BIAS ? table_stride(g) : 0;
+    const float* const my_bias = BIAS ? bias + kPad + (g.pack == 3 ? 4 * half * stride : 0) : nullptr;
+    const bool near = BIAS && first_tok - (key0 + 31) < g.far, edge = key0 + 31 > first_tok;
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const float4 lse4 = *reinterpret_cast<const float4*>(lse_t + b0 + 8 * a + 4 * half);
+      const float4 delta4 = *reinterpret_cast<const float4*>(lse_t + kRows + b0 + 8 * a + 4 * half);
+      const float lse[4] = {lse4.x, lse4.y, lse4.z, lse4.w}, delta[4] = {delta4.x, delta4.y, delta4.z, delta4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * a + j, ahead = (8 * a + j) >> g.pack;
+        float offset = -lse[j];
+        if (BIAS) offset += my_bias[(j & (heads - 1)) * stride + (near ? apart + ahead : g.far)];
+        const float p = exp2_fast(__builtin_fmaf(s[i], scale2, offset));
+        const bool hidden = edge && apart + ahead < 0;
+        s[i] = hidden ? 0.f : p;
+        dp[i] = hidden ? 0.f : p * (dp[i] - delta[j]);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < L::kGroups; ++c) {
+      const typename Op::Frag p = Op::from_acc(s, c), ds = Op::from_acc(dp, c);
+#pragma unroll
+      for (int e = 0; e < DP / 32; ++e) {
+        Op::mma(dv[e], L::col_frag(gt, col_base, b0, c, e), p);
+        Op::mma(dk[e], L::col_frag(qt, col_base, b0, c, e), ds);
+      }
+    }
+  };
+
   bool spoilt = false;
+  float joined_k[DP / 8], joined_v[DP / 8];  // SPLIT: this lane's columns of its key
   for (bool clean = false;; clean = true) {
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = floatx16_t{};
-    load(0);
-    for (int it = 0; it < steps; ++it) {
-      T* const qt = lds + (it & 1) * 2 * kTileElems;
-      T* const gt = qt + kTileElems;
-      float* const lse_t = stats + (it & 1) * 2 * kRows;
-      float* const delta_t = lse_t + kRows;
-      if (clean) {
-        sq.template store<true>(qt);
-        sg.template store<true>(gt);
+    if constexpr (SPLIT) {
+      T* const mine = lds + wave * 2 * kTileElems;
+      float* const stat = stats + wave * 2 * kRows;
+      const auto range = [&](int first, int end) {
+        if (first + wave < end) load(first + wave);
+        for (int it = first + wave; it < end; it += kWaves) {
+          wave_fence();
+          store(mine, stat, clean);
+          wave_fence();
+          if (it + kWaves < end) load(it + kWaves);
+          attend(mine, mine + kTileElems, stat, 0, first_row + it % tiles * kRows);
+        }
+      };
+      if (BIAS) {
+        for (int sub = 0; sub < subs; ++sub) {
+          __syncthreads();  // (the heads before are done with their bias)
+          fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
+          __syncthreads();
+          range(sub * tiles, (sub + 1) * tiles);
+        }
       } else {
-        sq.template store<false>(qt);
-        sg.template store<false>(gt);
+        range(0, steps);
       }
-      if (threadIdx.x < kRows) {
-        lse_t[threadIdx.x] = next_lse;
-        delta_t[threadIdx.x] = next_delta;
-      }
-      const int sub = it / tiles, r0 = first_row + it % tiles * kRows;
-      if (BIAS && it % tiles == 0) {
-        __syncthreads();  // (the last tile of the heads before is done with their bias)
-        fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
-      }
+      float* const parts = reinterpret_cast<float*>(smem_raw);
+      constexpr size_t kPart = 2 * kTileElems * sizeof(T) / sizeof(float);
+      static_assert(32 * DP <= kPart, "the parts take the tiles' place");
       __syncthreads();
-      if (it + 1 < steps) load(it + 1);
-#pragma unroll
-      for (int b = 0; b < kRows / 32; ++b) {
-        const int b0 = r0 + 32 * b, first_tok = b0 >> g.pack, last_tok = (b0 + 31) >> g.pack;
-        if (last_tok < key0) continue;
-        floatx16_t s{}, dp{};
-#pragma unroll
-        for (int c = 0; c < L::kSteps; ++c) Op::mma(s, L::row_frag(qt, 32 * b, c, lane), kf[c]);
-#pragma unroll
-        for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, L::row_frag(gt, 32 * b, c, lane), vf[c]);
-        // register i: token first_tok + (i's part, the same for all lanes) + (4 half >> pack), head likewise
-        const int apart = first_tok + ((4 * half) >> g.pack) - key;
-        const int stride = BIAS ? table_stride(g) : 0;
-        const float* const my_bias = BIAS ? bias + kPad + (g.pack == 3 ? 4 * half * stride : 0) : nullptr;
-        const bool near = BIAS && first_tok - (key0 + 31) < g.far, edge = key0 + 31 > first_tok;
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const float4 lse4 = *reinterpret_cast<const float4*>(lse_t + 32 * b + 8 * a + 4 * half);
-          const float4 delta4 = *reinterpret_cast<const float4*>(delta_t + 32 * b + 8 * a + 4 * half);
-          const float lse[4] = {lse4.x, lse4.y, lse4.z, lse4.w}, delta[4] = {delta4.x, delta4.y, delta4.z, delta4.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = 4 * a + j, ahead = (8 * a + j) >> g.pack;
-            float offset = -lse[j];
-            if (BIAS) offset += my_bias[(j & (heads - 1)) * stride + (near ? apart + ahead : g.far)];
-            const float p = exp2_fast(__builtin_fmaf(s[i], scale2, offset));
-            const bool hidden = edge && apart + ahead < 0;
-            s[i] = hidden ? 0.f : p;
-            dp[i] = hidden ? 0.f : p * (dp[i] - delta[j]);
-          }
+      write_part<DP>(parts + wave * kPart, dv, 1.f, lane);
+      __syncthreads();
+      join_parts<DP>(parts, kPart, wave, lane, joined_v);
+      __syncthreads();
+      write_part<DP>(parts + wave * kPart, dk, 1.f, lane);
+      __syncthreads();
+      join_parts<DP>(parts, kPart, wave, lane, joined_k);
+    } else {
+      load(0);
+      for (int it = 0; it < steps; ++it) {
+        T* const tile = lds + (it & 1) * 2 * kTileElems;
+        float* const stat = stats + (it & 1) * 2 * kRows;
+        store(tile, stat, clean);
+        const int sub = it / tiles, r0 = first_row + it % tiles * kRows;
+        if (BIAS && it % tiles == 0) {
+          __syncthreads();  // (the last tile of the heads before is done with their bias)
+          fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
         }
+        __syncthreads();
+        if (it + 1 < steps) load(it + 1);
 #pragma unroll
-        for (int c = 0; c < L::kGroups; ++c) {
-          const typename Op::Frag p = Op::from_acc(s, c), ds = Op::from_acc(dp, c);
-#pragma unroll
-          for (int e = 0; e < DP / 32; ++e) {
-            Op::mma(dv[e], L::col_frag(gt, 32 * b, c, 32 * e, lane), p);
-            Op::mma(dk[e], L::col_frag(qt, 32 * b, c, 32 * e, lane), ds);
-          }
-        }
+        for (int b = 0; b < kRows / 32; ++b)
+          if ((r0 + 32 * b + 31) >> g.pack >= key0) attend(tile, tile + kTileElems, stat, 32 * b, r0 + 32 * b);
       }
     }
     if (clean) break;
     float check = 0.f;
+    if constexpr (SPLIT) {
+#pragma unroll
+      for (int c = 0; c < DP / 8; ++c) check = __builtin_fmaf(joined_k[c], 0.f, __builtin_fmaf(joined_v[c], 0.f, check));
+    } else {
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) check = __builtin_fmaf(dk[b][i], 0.f, __builtin_fmaf(dv[b][i], 0.f, check));
-    check += other_half(check);
+    }
+    check = sum_of_halves(check);
     spoilt = there && check != 0.f;
     if (!__syncthreads_or(spoilt)) break;
   }
   T* const dk_rows = static_cast<T*>(g.dk) + w.start * g.dk_stride + static_cast<long long>(kv) * g.d;
   T* const dv_rows = static_cast<T*>(g.dv) + w.start * g.dv_stride + static_cast<long long>(kv) * g.d;
   if (there) {
+    if constexpr (SPLIT) {
+      store_joined<T, DP>(dk_rows + key * g.dk_stride, join_column<DP>(wave, lane), g.d, joined_k, g.scale);
+      store_joined<T, DP>(dv_rows + key * g.dv_stride, join_column<DP>(wave, lane), g.d, joined_v, 1.f);
+    }
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
+    for (int b = 0; b < (SPLIT ? 0 : DP / 32); ++b)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const int col = 32 * b + acc_row(i, half);
@@ -425,8 +541,10 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
         store4(dv_rows + key * g.dv_stride + col, dv[b][i], dv[b][i + 1], dv[b][i + 2], dv[b][i + 3]);
       }
   }
-  if (__any(spoilt)) __threadfence();
-  for (uint32_t keys = static_cast<uint32_t>(__ballot(spoilt)); keys != 0; keys &= keys - 1) {
+  uint32_t spoilt_keys = static_cast<uint32_t>(__ballot(spoilt));
+  if constexpr (SPLIT) spoilt_keys = share_rows(spoilt_keys, reinterpret_cast<uint32_t*>(stats + 2 * kWaves * kRows), wave);
+  if (spoilt_keys != 0) __threadfence();
+  for (uint32_t keys = spoilt_keys; keys != 0; keys &= keys - 1) {
     const int j = key0 + __builtin_ctz(keys);
     sum_key(g, w, kv, j, BIAS ? bias : nullptr, dk_rows + j * g.dk_stride, dv_rows + j * g.dv_stride);
   }
@@ -448,21 +566,17 @@ __global__ __launch_bounds__(kTableWaves * kWave) void attn_packed_table_kernel(
   store1(d_table + static_cast<long long>(b) * heads + h, sum);
 }
 
-template <typename Kernel>
-hipError_t launch(Kernel kern, size_t groups, size_t lds, const PackedAttn& g, hipStream_t st) {
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(groups)), dim3(kThreads), lds, st, g);
-  return hipGetLastError();
-}
 template <typename T, int DP, bool BIAS>
 hipError_t launch_bwd(const PackedAttn& g, hipStream_t st) {
-  const size_t slots = attn_packed_row_slots(g), table = BIAS ? static_cast<size_t>(table_floats(g)) * sizeof(float) : 0;
-  const size_t by_row = BIAS ? g.buckets * kHistStride * sizeof(float) + table_stride(g) : 0;
-  hipError_t e = launch(attn_packed_rows_kernel<T, DP, BIAS>, slots * (g.heads >> g.pack), Rows<T, DP, BIAS>::kLds + table + by_row, g, st);
+  const size_t table = BIAS ? static_cast<size_t>(table_floats(g)) * sizeof(float) : 0;
+  const size_t by_row = table + (BIAS ? kWaves * by_distance_floats(g) * sizeof(float) : 0);
+  const size_t slots = attn_packed_row_slots(g, g.split_rows), key_groups = attn_packed_key_slots(g) * g.kv_heads;
+  const size_t row_groups = slots * (g.heads >> g.pack);
+  hipError_t e = g.split_rows ? launch_packed<attn_packed_rows_kernel<T, DP, BIAS, true>>(row_groups, Rows<T, DP, BIAS, true>::kLds + by_row, g, st)
+                              : launch_packed<attn_packed_rows_kernel<T, DP, BIAS, false>>(row_groups, Rows<T, DP, BIAS, false>::kLds + by_row, g, st);
   if (e != hipSuccess) return e;
-  const size_t key_slots = (static_cast<size_t>(g.tokens) >> kRowsLog) + g.sequences;
-  e = launch(attn_packed_keys_kernel<T, DP, BIAS>, key_slots * g.kv_heads, Keys<T, DP>::kLds + table, g, st);
+  e = g.split_keys ? launch_packed<attn_packed_keys_kernel<T, DP, BIAS, true>>(key_groups, Keys<T, DP, true>::kLds + table, g, st)
+                   : launch_packed<attn_packed_keys_kernel<T, DP, BIAS, false>>(key_groups, Keys<T, DP, false>::kLds + table, g, st);
   if (e != hipSuccess || !BIAS) return e;
   hipLaunchKernelGGL((attn_packed_table_kernel<T>), dim3(g.heads), dim3(kTableWaves * kWave), 0, st, g.partials, static_cast<T*>(g.d_table),
                      static_cast<int>(slots), g.heads, g.buckets);
@@ -479,6 +593,11 @@ hipError_t launch_bwd(const PackedAttn& g, hipStream_t st) {
 
 }  // namespace
 
+bool attn_packed_split_rows_fit(int dtype, const PackedAttn& g) {
+  const size_t tiles = dtype == 1 ? (g.d <= 64 ? Rows<bf16_t, 64, true, true>::kLds : Rows<bf16_t, 128, true, true>::kLds)
+                                  : (g.d <= 64 ? Rows<float, 64, true, true>::kLds : Rows<float, 128, true, true>::kLds);
+  return g.buckets == 0 || tiles + (table_floats(g) + kWaves * by_distance_floats(g)) * sizeof(float) <= kMostLds;
+}
 hipError_t attn_packed_bwd(int dtype, const PackedAttn& g, hipStream_t st) {
   return dtype == 1 ? launch_bwd<bf16_t>(g, st) : launch_bwd<float>(g, st);
 }

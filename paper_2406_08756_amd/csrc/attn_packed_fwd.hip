@@ -5,10 +5,12 @@
 namespace lynx {
 namespace {
 
-template <typename T, int DP> struct Fwd {
-  static constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;  // keys per tile
-  static constexpr size_t kTileBytes = static_cast<size_t>(kKeys) * DP * sizeof(T);
-  static constexpr size_t kLds = 4 * kTileBytes;  // K and V, two of each
+template <typename T, int DP, bool SPLIT> struct Fwd {
+  static constexpr int kKeys = sizeof(T) == 2 && !SPLIT ? 64 : 32;  // keys per tile
+  static constexpr int kTileElems = kKeys * DP;
+  // K and V, two of each, or one of each wavefront
+  static constexpr size_t kTiles = (SPLIT ? 2 * kWaves : 4) * static_cast<size_t>(kTileElems) * sizeof(T);
+  static constexpr size_t kLds = kTiles + (SPLIT ? 2 * kWaves * 32 * sizeof(float) : 0);
 };
 
 // One row again, pair by pair: lanes take keys for the scores and columns for the sum.
@@ -41,15 +43,15 @@ __device__ void sum_row_forward(const PackedAttn& g, const T* q, const T* k, con
     if (lane + kWave * c < g.d) store1(out + lane + kWave * c, acc[c]);
 }
 
-template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__(kThreads, 2) void attn_packed_fwd_kernel(PackedAttn g) {
+template <typename T, int DP, bool BIAS, bool SPLIT>
+__global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) void attn_packed_fwd_kernel(PackedAttn g) {
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
-  typedef Fwd<T, DP> S;
-  constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32;
+  typedef Fwd<T, DP, SPLIT> S;
+  constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32, kTileElems = S::kTileElems, kRowsLog = rows_log(SPLIT);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   T* const lds = reinterpret_cast<T*>(smem_raw);
-  constexpr int kTileElems = kKeys * DP;
+  float* const tops = reinterpret_cast<float*>(smem_raw + S::kTiles);  // SPLIT: each wavefront's maxima and sums
   float* const bias = reinterpret_cast<float*>(smem_raw + S::kLds);
 
   const int subs = g.heads >> g.pack;
@@ -67,7 +69,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_packed_fwd_kernel(PackedAttn
   const T* const v = static_cast<const T*>(g.v) + w.start * g.v_stride + static_cast<long long>(kv) * g.d;
   T* const out = static_cast<T*>(g.out) + w.start * g.out_stride + static_cast<long long>(head0) * g.d;
 
-  const int row0 = (w.tile << kRowsLog) + 32 * wave;  // this wavefront's
+  const int row0 = (w.tile << kRowsLog) + (SPLIT ? 0 : 32 * wave);  // this wavefront's
   const int row = row0 + (lane & 31), tok = row >> g.pack, hp = row & (heads - 1);
   const int first_tok = row0 >> g.pack, last_tok = first_tok < w.len ? min((row0 + 31) >> g.pack, w.len - 1) : -1;
   const bool there = tok < w.len;
@@ -80,133 +82,212 @@ __global__ __launch_bounds__(kThreads, 2) void attn_packed_fwd_kernel(PackedAttn
                                    left > 0 ? static_cast<uint32_t>((left - 1) * g.q_stride + heads * g.d) * static_cast<uint32_t>(sizeof(T)) : 0u);
     load_row_frags<T, DP>(b, (static_cast<uint32_t>(tok - first_tok) * static_cast<uint32_t>(g.q_stride) + hp * g.d) * static_cast<uint32_t>(sizeof(T)), g.d, lane, qf);
   }
-  const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);  // of the workgroup: the keys it sees
-  const int tiles = (end_tok + kKeys - 1) / kKeys;
   const float* const my_bias = BIAS ? bias + hp * table_stride(g) + kPad : nullptr;
+  if (SPLIT && BIAS) __syncthreads();
 
-  Stage<T, DP, kKeys, kThreads> sk, sv;
+  constexpr int kTogether = SPLIT ? kWave : kThreads;
+  const int who = SPLIT ? lane : static_cast<int>(threadIdx.x);
+  Stage<T, DP, kKeys, kTogether> sk, sv;
   floatx16_t o[DP / 32];
   float m, total;
+  const auto load = [&](int t) {
+    sk.load_keys(k, g.k_stride, t * kKeys, w.len, g.d, who);
+    sv.load_keys(v, g.v_stride, t * kKeys, w.len, g.d, who);
+  };
+  const auto store = [&](T* tile, bool clean) {
+    sk.template store<false>(tile, who);
+    if (clean) sv.template store<true>(tile + kTileElems, who);
+    else sv.template store<false>(tile + kTileElems, who);
+  };
+  const uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
+  // the keys from key0 on, at kt and vt, for this wavefront's rows
+  const auto attend = [&](const T* kt, const T* vt, int key0) {
+    typename Op::Frag rows[2][L::kSteps];
+    const auto read_rows = [&](int b) {
+#pragma unroll
+      for (int c = 0; c < L::kSteps; ++c) rows[b & 1][c] = L::row_frag(kt, row_base, 32 * b, c);
+    };
+    floatx16_t s[kBlocks];
+    read_rows(0);
+    requested();
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      if (b + 1 < kBlocks) read_rows(b + 1);
+      s[b] = floatx16_t{};
+#pragma unroll
+      for (int c = 0; c < L::kSteps; ++c) Op::mma(s[b], rows[b & 1][c], qf[c]);
+    }
+    // V's fragments are requested ahead of the arithmetic that its products wait for, as many as registers are free
+    constexpr int kAhead = sizeof(T) == 2 ? L::kGroups : 1;
+    typename Op::Frag vf[kAhead][DP / 32];
+    const auto read_values = [&](int b, int c0) {
+#pragma unroll
+      for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+        for (int e = 0; e < DP / 32; ++e) vf[c][e] = L::col_frag(vt, col_base, 32 * b, c0 + c, e);
+    };
+    read_values(0, 0);
+    requested();
+    float top = -kInf;
+    const bool edge = key0 + kKeys - 1 > first_tok;
+    if (BIAS) {
+      const int apart = tok - key0 - 4 * half;
+      if (first_tok - (key0 + kKeys - 1) < g.far) {
+        const float* const at = my_bias + apart;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            // (masked by a choice: the sum would be NaN where the score is)
+            const float z = __builtin_fmaf(s[b][i], scale2, at[-(32 * b + acc_row(i, 0))]);
+            s[b][i] = apart >= 32 * b + acc_row(i, 0) ? z : -kInf;
+            top = fmaxf(top, s[b][i]);
+          }
+      } else {
+        const float far = my_bias[g.far];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[b][i] = __builtin_fmaf(s[b][i], scale2, far);
+            top = fmaxf(top, s[b][i]);
+          }
+      }
+    } else {
+      if (edge) {
+        const int apart = tok - key0 - 4 * half;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (apart < 32 * b + acc_row(i, 0)) s[b][i] = -kInf;
+      }
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+      top *= scale2;
+    }
+    top = max_of_halves(top);
+    // The reference follows the maximum only where that has left it 2^8 behind: probabilities up to 256 lose nothing in
+    // fp32 sums or by a rounding to the storage type, and the accumulators are hardly ever scaled.  A row decides for itself:
+    // for the others of the wavefront the factor is 1.
+    if (__any(top > m + 8.f)) {
+      const float now = top > m + 8.f ? top : m;
+      const float shrink = now == m ? 1.f : exp2_fast(m - now);
+      m = now;
+      total *= shrink;
+#pragma unroll
+      for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] *= shrink;
+    }
+    const float base = m == -kInf ? 0.f : m;  // (a row that has seen nothing yet: every probability 0)
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = exp2_fast(BIAS ? s[b][i] - base : __builtin_fmaf(s[b][i], scale2, -base));
+        total += s[b][i];
+      }
+#pragma unroll
+      for (int c = 0; c < L::kGroups; ++c) {
+        if (c % kAhead == 0 && (b != 0 || c != 0)) read_values(b, c);
+        const typename Op::Frag p = Op::from_acc(s[b], c);
+#pragma unroll
+        for (int e = 0; e < DP / 32; ++e) Op::mma(o[e], vf[c % kAhead][e], p);
+      }
+    }
+  };
+
   bool spoilt = false;
+  float joined[DP / 8];  // SPLIT: this lane's columns of its row
   for (bool clean = false;; clean = true) {
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) o[b] = floatx16_t{};
     m = -kInf;       // maximum of the logits so far, times log2 e
     total = 0.f;     // this half's share of the sum
-    sk.load_keys(k, g.k_stride, 0, w.len, g.d);
-    sv.load_keys(v, g.v_stride, 0, w.len, g.d);
-    for (int t = 0; t < tiles; ++t) {
-      T* const kt = lds + (t & 1) * 2 * kTileElems;
-      T* const vt = kt + kTileElems;
-      sk.template store<false>(kt);
-      if (clean) sv.template store<true>(vt);
-      else sv.template store<false>(vt);
-      __syncthreads();
-      if (t + 1 < tiles) {
-        sk.load_keys(k, g.k_stride, (t + 1) * kKeys, w.len, g.d);
-        sv.load_keys(v, g.v_stride, (t + 1) * kKeys, w.len, g.d);
+    if constexpr (SPLIT) {
+      T* const mine = lds + wave * 2 * kTileElems;
+      const int tiles = last_tok / kKeys + 1;
+      if (wave < tiles) load(wave);
+      for (int t = wave; t < tiles; t += kWaves) {
+        wave_fence();
+        store(mine, clean);
+        wave_fence();
+        if (t + kWaves < tiles) load(t + kWaves);
+        attend(mine, mine + kTileElems, t * kKeys);
       }
-      const int key0 = t * kKeys;
-      if (key0 > last_tok) continue;
-      floatx16_t s[kBlocks];
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        s[b] = floatx16_t{};
-#pragma unroll
-        for (int c = 0; c < L::kSteps; ++c) Op::mma(s[b], L::row_frag(kt, 32 * b, c, lane), qf[c]);
-      }
-      float top = -kInf;
-      const bool edge = key0 + kKeys - 1 > first_tok;
-      if (BIAS) {
-        const int apart = tok - key0 - 4 * half;
-        if (first_tok - (key0 + kKeys - 1) < g.far) {
-          const float* const at = my_bias + apart;
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              // (masked by a choice: the sum would be NaN where the score is)
-              const float z = __builtin_fmaf(s[b][i], scale2, at[-(32 * b + acc_row(i, 0))]);
-              s[b][i] = apart >= 32 * b + acc_row(i, 0) ? z : -kInf;
-              top = fmaxf(top, s[b][i]);
-            }
-        } else {
-          const float far = my_bias[g.far];
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              s[b][i] = __builtin_fmaf(s[b][i], scale2, far);
-              top = fmaxf(top, s[b][i]);
-            }
-        }
-      } else {
-        if (edge) {
-          const int apart = tok - key0 - 4 * half;
-#pragma unroll
-          for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (apart < 32 * b + acc_row(i, 0)) s[b][i] = -kInf;
-        }
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top *= scale2;
-      }
-      top = fmaxf(top, other_half(top));
-      if (__any(top > m)) {
-        const float now = fmaxf(top, m);
-        const float shrink = now == -kInf ? 1.f : exp2_fast(m - now);
-        m = now;
-        total *= shrink;
-#pragma unroll
-        for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[b][i] *= shrink;
-      }
-      const float base = m == -kInf ? 0.f : m;  // (a row that has seen nothing yet: every probability 0)
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[b][i] = exp2_fast(BIAS ? s[b][i] - base : __builtin_fmaf(s[b][i], scale2, -base));
-          total += s[b][i];
-        }
-#pragma unroll
-        for (int c = 0; c < L::kGroups; ++c) {
-          const typename Op::Frag p = Op::from_acc(s[b], c);
-#pragma unroll
-          for (int e = 0; e < DP / 32; ++e) Op::mma(o[e], L::col_frag(vt, 32 * b, c, 32 * e, lane), p);
-        }
+    } else {
+      const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);  // of the workgroup: the keys it sees
+      const int tiles = (end_tok + kKeys - 1) / kKeys;
+      load(0);
+      for (int t = 0; t < tiles; ++t) {
+        T* const tile = lds + (t & 1) * 2 * kTileElems;
+        store(tile, clean);
+        __syncthreads();
+        if (t + 1 < tiles) load(t + 1);
+        if (t * kKeys <= last_tok) attend(tile, tile + kTileElems, t * kKeys);
       }
     }
-    total += other_half(total);
+
+    total = sum_of_halves(total);
+    if constexpr (SPLIT) {
+      if (half == 0) {
+        tops[wave * 32 + lane] = m;
+        tops[(kWaves + wave) * 32 + lane] = total;
+      }
+      __syncthreads();
+      float top = -kInf, own = m;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) top = fmaxf(top, tops[i * 32 + (lane & 31)]);
+      total = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        const float of = tops[i * 32 + (lane & 31)];
+        // (a wavefront whose keys this row does not see has an empty part)
+        total += of == -kInf ? tops[(kWaves + i) * 32 + (lane & 31)] : tops[(kWaves + i) * 32 + (lane & 31)] * exp2_fast(of - top);
+      }
+      m = top;
+      constexpr size_t kPartFloats = static_cast<size_t>(DP) * 32;
+      float* const parts = reinterpret_cast<float*>(smem_raw);
+      static_assert(kWaves * kPartFloats * sizeof(float) <= S::kTiles, "the parts take the tiles' place");
+      write_part<DP>(parts + wave * (2 * kTileElems * sizeof(T) / sizeof(float)), o, own == -kInf ? 1.f : exp2_fast(own - top), lane);
+      __syncthreads();
+      join_parts<DP>(parts, 2 * kTileElems * sizeof(T) / sizeof(float), wave, lane, joined);
+    }
     if (clean) break;
     float check = total * 0.f;
+    if constexpr (SPLIT) {
+#pragma unroll
+      for (int c = 0; c < DP / 8; ++c) check = __builtin_fmaf(joined[c], 0.f, check);
+    } else {
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) check = __builtin_fmaf(o[b][i], 0.f, check);
-    check += other_half(check);
+    }
+    check = sum_of_halves(check);
     spoilt = there && check != 0.f;
     if (!__syncthreads_or(spoilt)) break;
   }
   const float inverse = total == 0.f ? 0.f : 1.f / total;
   T* const mine = out + tok * g.out_stride + hp * g.d;
+  if (SPLIT && there) store_joined<T, DP>(mine, join_column<DP>(wave, lane), g.d, joined, inverse);
   if (there) {
-    if (half == 0) g.lse[static_cast<long long>(head0 + hp) * g.tokens + w.start + tok] = (m + __builtin_log2f(total)) * kLn2;
+    if (half == 0 && (!SPLIT || wave == 0)) g.lse[static_cast<long long>(head0 + hp) * g.tokens + w.start + tok] = (m + __builtin_log2f(total)) * kLn2;
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
+    for (int b = 0; b < (SPLIT ? 0 : DP / 32); ++b)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const int col = 32 * b + acc_row(i, half);
         if (col < g.d) store4(mine + col, o[b][i] * inverse, o[b][i + 1] * inverse, o[b][i + 2] * inverse, o[b][i + 3] * inverse);
       }
   }
-  if (__any(spoilt)) __threadfence();
-  for (uint32_t rows = static_cast<uint32_t>(__ballot(spoilt)); rows != 0; rows &= rows - 1) {
+  uint32_t rows = static_cast<uint32_t>(__ballot(spoilt));
+  if constexpr (SPLIT) rows = share_rows(rows, reinterpret_cast<uint32_t*>(tops), wave);
+  if (rows != 0) __threadfence();
+  for (; rows != 0; rows &= rows - 1) {
     const int r = __builtin_ctz(rows), t = (row0 + r) >> g.pack, h = (row0 + r) & (heads - 1);
     sum_row_forward(g, q + t * g.q_stride + h * g.d, k, v, t, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(m), r)),
                     __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(total), r)), scale2,
@@ -216,12 +297,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_packed_fwd_kernel(PackedAttn
 
 template <typename T, int DP, bool BIAS>
 hipError_t launch_fwd(const PackedAttn& g, hipStream_t st) {
-  const size_t lds = Fwd<T, DP>::kLds + (BIAS ? static_cast<size_t>(table_floats(g)) * sizeof(float) : 0);
-  const auto kern = attn_packed_fwd_kernel<T, DP, BIAS>;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(attn_packed_row_slots(g) * (g.heads >> g.pack))), dim3(kThreads), lds, st, g);
-  return hipGetLastError();
+  const size_t table = BIAS ? static_cast<size_t>(table_floats(g)) * sizeof(float) : 0;
+  const size_t groups = attn_packed_row_slots(g, g.split_fwd) * (g.heads >> g.pack);
+  return g.split_fwd ? launch_packed<attn_packed_fwd_kernel<T, DP, BIAS, true>>(groups, Fwd<T, DP, true>::kLds + table, g, st)
+                      : launch_packed<attn_packed_fwd_kernel<T, DP, BIAS, false>>(groups, Fwd<T, DP, false>::kLds + table, g, st);
 }
 template <typename T, int DP>
 hipError_t launch_fwd(const PackedAttn& g, hipStream_t st) {
@@ -234,19 +313,28 @@ hipError_t launch_fwd(const PackedAttn& g, hipStream_t st) {
 
 }  // namespace
 
-// As many heads of a group as are a power of two, up to 8; fewer where their biases by distance would take more than 24 KB
-// of LDS (with the histograms of the backward pass in fp32, what is left of it).
-void attn_packed_choose_pack(PackedAttn* g) {
+// Fewer workgroups of 128 rows or keys than this, and 32 each go faster.
+constexpr size_t kSplitBelow = 512;
+// As many heads of a group as are a power of two, up to 8; fewer where their biases by distance would take more than 10 KB of
+// LDS, so that with four times that for the gradient's sums and the tiles of fp32 a workgroup has what it needs.
+void attn_packed_choose(int dtype, PackedAttn* g) {
   const int group = g->heads / g->kv_heads;
   g->pack = 0;
-  while (g->pack < 3 && (group >> g->pack) % 2 == 0 && (g->buckets == 0 || table_stride(*g) << (g->pack + 1) <= 6144)) ++g->pack;
+  while (g->pack < 3 && (group >> g->pack) % 2 == 0 && (g->buckets == 0 || table_stride(*g) << (g->pack + 1) <= 2560)) ++g->pack;
+  g->split_fwd = attn_packed_row_slots(*g, false) * (g->heads >> g->pack) < kSplitBelow;
+  g->split_rows = g->split_fwd && attn_packed_split_rows_fit(dtype, *g);
+  g->split_keys = 0;
+  g->split_keys = attn_packed_key_slots(*g) * g->kv_heads < kSplitBelow;
 }
 bool attn_packed_fits(const PackedAttn& g) {
-  const long long slots = static_cast<long long>(attn_packed_row_slots(g));
+  const long long slots = static_cast<long long>(attn_packed_row_slots(g, g.split_fwd));
   return fits_grid(slots * (g.heads >> g.pack), kThreads) && slots < (1ll << 31);
 }
-size_t attn_packed_row_slots(const PackedAttn& g) {
-  return ((static_cast<size_t>(g.tokens) << g.pack) >> kRowsLog) + static_cast<size_t>(g.sequences);
+size_t attn_packed_row_slots(const PackedAttn& g, bool split) {
+  return ((static_cast<size_t>(g.tokens) << g.pack) >> rows_log(split)) + static_cast<size_t>(g.sequences);
+}
+size_t attn_packed_key_slots(const PackedAttn& g) {
+  return (static_cast<size_t>(g.tokens) >> rows_log(g.split_keys)) + static_cast<size_t>(g.sequences);
 }
 hipError_t attn_packed_fwd(int dtype, const PackedAttn& g, hipStream_t st) {
   return dtype == 1 ? launch_fwd<bf16_t>(g, st) : launch_fwd<float>(g, st);

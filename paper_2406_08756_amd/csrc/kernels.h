@@ -244,16 +244,19 @@ struct PackedAttn {
   long long q_stride, k_stride, v_stride, out_stride, dq_stride, dk_stride, dv_stride;  // elements between tokens
   int sequences, tokens, heads, kv_heads, d;
   int pack;                // log2 of the query heads whose rows share a tile
+  int split_fwd, split_rows, split_keys;  // 32 rows (keys) per workgroup instead of 128: forward and the two backward kernels
   float scale;
   int buckets, far;        // far: the distance from which on the last bucket holds, at least 1
-  int starts[kMaxBuckets];
+  int starts[kMaxBuckets];  // first distance of each bucket; behind the last one the largest number
 };
 hipError_t attn_packed_fwd(int dtype, const PackedAttn& g, hipStream_t st);
 hipError_t attn_packed_bwd(int dtype, const PackedAttn& g, hipStream_t st);
-// Sets `pack` from the heads and the position bias.
-void attn_packed_choose_pack(PackedAttn* g);
-// Row tiles that a launch has room for: `partials` holds [row slots, heads, buckets].
-size_t attn_packed_row_slots(const PackedAttn& g);
+// Sets `pack` and the splits from the shape.
+void attn_packed_choose(int dtype, PackedAttn* g);
+bool attn_packed_split_rows_fit(int dtype, const PackedAttn& g);
+// Tiles that a launch has room for; `partials` holds [row slots of split_rows, heads, buckets].
+size_t attn_packed_row_slots(const PackedAttn& g, bool split);
+size_t attn_packed_key_slots(const PackedAttn& g);
 // Whether its launches have few enough workgroups.
 bool attn_packed_fits(const PackedAttn& g);
 

@@ -34,7 +34,7 @@ SHAPES = [
     (1, 1, 16, [0, 0, 5, 0], {}),
     (4, 1, 64, [2] * 150 + [0] * 30 + [9], {}),
 ]
-BIASES = [None, ("usual", 32, 128), ("starts", [0]), ("starts", [0, 0, 1, 1, 40]), ("usual", 64, 1024), ("usual", 9, 4096)]
+BIASES = [None, ("usual", 32, 128), ("starts", [0]), ("starts", [0, 0, 1, 1, 40]), ("usual", 64, 1024), ("usual", 9, 2048)]
 
 
 def starts_of(bias):
