@@ -217,43 +217,59 @@ template <typename T, int DP> struct Tile {
 // Byte offset that every row buffer reads as zero.
 constexpr uint32_t kOutside = 0x80000000u;
 
-// ROWS rows on their way from memory to a tile: requested into registers, stored when the tile is free.
-// THREADS threads (`who` of them) do it together.
+// One 16-byte load per lane straight into LDS, at `to` (uniform) + 16 lane; outside the buffer it stores zeros.  Written out
+// because the compiler takes every LDS read behind such a load, as a builtin, to wait for it: here a tile is read while the
+// next one is on its way.  The load has no result register; landed() is the wait, and other wavefronts need a barrier after
+// it.  (Loads that the compiler counts are only waited for the longer.)
+__device__ __forceinline__ void load_to_lds(const RowBuffer& b, uint32_t offset, const void* to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef const __attribute__((address_space(3))) void* lds_ptr_t;
+  const uint32_t at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)(to))));
+  uint32_t kept;  // (M0, which the load takes its place from, is the compiler's)
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(kept) : "s"(at), "v"(offset), "s"(b.rsrc) : "memory");
+#endif
+}
+// Waits until at most N of this wavefront's loads are in flight; with LDS, until its LDS accesses are done too.
+template <int N>
+__device__ __forceinline__ void landed() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// ROWS rows to a tile by THREADS threads (`wave`: which wavefront of them).
 template <typename T, int DP, int ROWS, int THREADS> struct Stage {
   typedef Tile<T, DP> L;
   static constexpr int kLoads = ROWS * L::kChunks / THREADS;
-  static_assert(ROWS * L::kChunks % THREADS == 0, "a tile splits over the threads");
-  uintx4_t v[kLoads];
-  // keys: rows first.. of `base` (row 0's first element), `rows` of which exist
-  __device__ __forceinline__ void load_keys(const T* base, long long stride, int first, int rows, int d, int who) {
+  static_assert(ROWS * L::kChunks % THREADS == 0 && THREADS % kWave == 0, "a tile splits over the wavefronts");
+  // keys: rows first.. of `base` (row 0's first element), `rows` of which exist; zeros behind them and behind column d
+  __device__ static __forceinline__ void keys(T* tile, const T* base, long long stride, int first, int rows, int d, int wave, int lane) {
     const int left = min(rows - first, ROWS);
     const RowBuffer b = row_buffer(base + first * stride, left > 0 ? static_cast<uint32_t>((left - 1) * stride + d) * static_cast<uint32_t>(sizeof(T)) : 0u);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int e = who + THREADS * j, row = e / L::kChunks, col = e % L::kChunks * L::kChunk;
+      const int e = wave * kWave + lane + THREADS * j, row = e / L::kChunks, col = (e % L::kChunks ^ L::swizzle(row)) * L::kChunk;
       const uint32_t off = (static_cast<uint32_t>(row) * static_cast<uint32_t>(stride) + col) * static_cast<uint32_t>(sizeof(T));
-      v[j] = row_buffer_load(b, col < d ? off : kOutside);
+      load_to_lds(b, col < d ? off : kOutside, tile + (wave * kWave + THREADS * j) * L::kChunk);
     }
   }
   // the same of rows that are (token, head) pairs; `first` is a whole token's
-  __device__ __forceinline__ void load_rows(const T* base, long long stride, int first, int tokens, int d, int pack, int who) {
+  __device__ static __forceinline__ void rows(T* tile, const T* base, long long stride, int first, int tokens, int d, int pack, int wave, int lane) {
     const int token = first >> pack, left = min(tokens - token, max(ROWS >> pack, 1)), heads = 1 << pack;
     const RowBuffer b = row_buffer(base + token * stride, left > 0 ? static_cast<uint32_t>((left - 1) * stride + heads * d) * static_cast<uint32_t>(sizeof(T)) : 0u);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int e = who + THREADS * j, row = e / L::kChunks, col = e % L::kChunks * L::kChunk;
+      const int e = wave * kWave + lane + THREADS * j, row = e / L::kChunks, col = (e % L::kChunks ^ L::swizzle(row)) * L::kChunk;
       const uint32_t off = (static_cast<uint32_t>(row >> pack) * static_cast<uint32_t>(stride) + (row & (heads - 1)) * d + col) * static_cast<uint32_t>(sizeof(T));
-      v[j] = row_buffer_load(b, col < d ? off : kOutside);
+      load_to_lds(b, col < d ? off : kOutside, tile + (wave * kWave + THREADS * j) * L::kChunk);
     }
   }
-  template <bool CLEAN>
-  __device__ __forceinline__ void store(T* tile, int who) {
+  // what this lane has loaded, without infinities and NaN
+  __device__ static __forceinline__ void clean(T* tile, int wave, int lane) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int e = who + THREADS * j;
-      uintx4_t w = v[j];
-      if (CLEAN) w = without_nonfinite(w, static_cast<const T*>(nullptr));
-      *reinterpret_cast<uintx4_t*>(tile + L::at(e / L::kChunks, e % L::kChunks)) = w;
+      uintx4_t* const p = reinterpret_cast<uintx4_t*>(tile + (wave * kWave + lane + THREADS * j) * L::kChunk);
+      *p = without_nonfinite(*p, static_cast<const T*>(nullptr));
     }
   }
 };

@@ -133,26 +133,36 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   if (SPLIT && BIAS) __syncthreads();
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
-  const int who = SPLIT ? lane : static_cast<int>(threadIdx.x);
-  Stage<T, DP, kKeys, kTogether> sk, sv;
+  typedef Stage<T, DP, kKeys, kTogether> Load;
+  const int part = SPLIT ? 0 : wave;  // of a tile's load
   floatx16_t acc[DP / 32];
-  const auto load = [&](int t) {
-    sk.load_keys(k, g.k_stride, t * kKeys, w.len, g.d, who);
-    sv.load_keys(v, g.v_stride, t * kKeys, w.len, g.d, who);
-  };
-  const auto store = [&](T* tile, bool clean) {
-    if (clean) sk.template store<true>(tile, who);
-    else sk.template store<false>(tile, who);
-    sv.template store<false>(tile + kTileElems, who);
-  };
+  const auto load_k = [&](T* tile, int t) { Load::keys(tile, k, g.k_stride, t * kKeys, w.len, g.d, part, lane); };
+  const auto load_v = [&](T* tile, int t) { Load::keys(tile, v, g.v_stride, t * kKeys, w.len, g.d, part, lane); };
   const uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
-  // 32 keys from key0 on, rows b0.. of kt and vt
-  const auto attend = [&](const T* kt, const T* vt, int b0, int key0, bool clean) {
+  // 32 keys from key0 on, rows b0.. of kt and vt.  v_read() is called when V's have been read.
+  const auto attend = [&](const T* kt, const T* vt, int b0, int key0, bool clean, auto&& v_read) {
+    typename Op::Frag k_rows[L::kSteps], v_rows[L::kSteps];
+#pragma unroll
+    for (int c = 0; c < L::kSteps; ++c) k_rows[c] = L::row_frag(kt, row_base, b0, c);
+#pragma unroll
+    for (int c = 0; c < L::kSteps; ++c) v_rows[c] = L::row_frag(vt, row_base, b0, c);
+    requested();
     floatx16_t s{}, dp{};
 #pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) Op::mma(s, L::row_frag(kt, row_base, b0, c), qf[c]);
+    for (int c = 0; c < L::kSteps; ++c) Op::mma(s, k_rows[c], qf[c]);
 #pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, L::row_frag(vt, row_base, b0, c), gf[c]);
+    for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, v_rows[c], gf[c]);
+    v_read();
+    constexpr int kAhead = sizeof(T) == 2 ? L::kGroups : 1;
+    typename Op::Frag k_cols[kAhead][DP / 32];
+    const auto read_cols = [&](int c0) {
+#pragma unroll
+      for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+        for (int e = 0; e < DP / 32; ++e) k_cols[c][e] = L::col_frag(kt, col_base, b0, c0 + c, e);
+    };
+    read_cols(0);
+    requested();
     const int apart = tok - key0 - 4 * half;
     const bool near = BIAS && first_tok - (key0 + 31) < g.far, edge = key0 + 31 > first_tok;
     const float offset = BIAS && !near ? lse2 - my_bias[g.far] : lse2;
@@ -196,9 +206,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
     }
 #pragma unroll
     for (int c = 0; c < L::kGroups; ++c) {
+      if (c != 0 && c % kAhead == 0) read_cols(c);
       const typename Op::Frag ds = Op::from_acc(s, c);
 #pragma unroll
-      for (int e = 0; e < DP / 32; ++e) Op::mma(acc[e], L::col_frag(kt, col_base, b0, c, e), ds);
+      for (int e = 0; e < DP / 32; ++e) Op::mma(acc[e], k_cols[c % kAhead][e], ds);
     }
   };
 
@@ -208,15 +219,24 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) acc[b] = floatx16_t{};
     if constexpr (SPLIT) {
-      T* const mine = lds + wave * 2 * kTileElems;
+      // one tile of each: V's next one is requested when it has been read, K's at the end
+      T* const kt = lds + wave * 2 * kTileElems;
+      T* const vt = kt + kTileElems;
       const int tiles = last_tok / kKeys + 1;
-      if (wave < tiles) load(wave);
+      if (wave < tiles) {
+        load_v(vt, wave);
+        load_k(kt, wave);
+      }
       for (int t = wave; t < tiles; t += kWaves) {
-        wave_fence();
-        store(mine, clean);
-        wave_fence();
-        if (t + kWaves < tiles) load(t + kWaves);
-        attend(mine, mine + kTileElems, 0, t * kKeys, clean);
+        const bool more = t + kWaves < tiles;
+        landed<0>();
+        if (clean) Load::clean(kt, 0, lane);
+        attend(kt, vt, 0, t * kKeys, clean, [&] {
+          lds_done();
+          if (more) load_v(vt, t + kWaves);
+        });
+        lds_done();
+        if (more) load_k(kt, t + kWaves);
       }
       __syncthreads();
       float* const parts = reinterpret_cast<float*>(smem_raw);
@@ -228,15 +248,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
     } else {
       const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);
       const int tiles = (end_tok + kKeys - 1) / kKeys;
-      load(0);
+      load_k(lds, 0);
+      load_v(lds + kTileElems, 0);
       for (int t = 0; t < tiles; ++t) {
         T* const tile = lds + (t & 1) * 2 * kTileElems;
-        store(tile, clean);
+        landed<0>();
+        if (clean) Load::clean(tile, part, lane);
         __syncthreads();
-        if (t + 1 < tiles) load(t + 1);
+        if (t + 1 < tiles) {
+          T* const next = lds + (~t & 1) * 2 * kTileElems;
+          load_k(next, t + 1);
+          load_v(next + kTileElems, t + 1);
+        }
 #pragma unroll
         for (int b = 0; b < kKeys / 32; ++b)
-          if (t * kKeys + 32 * b <= last_tok) attend(tile, tile + kTileElems, 32 * b, t * kKeys + 32 * b, clean);
+          if (t * kKeys + 32 * b <= last_tok) attend(tile, tile + kTileElems, 32 * b, t * kKeys + 32 * b, clean, [] {});
       }
     }
     if (clean) break;
@@ -378,15 +404,18 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
   const int tiles = (rows - first_row + kRows - 1) / kRows, steps = tiles * subs;
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
+  typedef Stage<T, DP, kRows, kTogether> Load;
+  const int part = SPLIT ? 0 : wave;  // of a tile's load
   const int who = SPLIT ? lane : static_cast<int>(threadIdx.x);
-  Stage<T, DP, kRows, kTogether> sq, sg;
   float next_lse = kInf, next_delta = 0.f;
-  const auto load = [&](int it) {
+  const auto load = [&](T* tile, int it) {
     const int sub = it / tiles, r0 = first_row + it % tiles * kRows;
-    sq.load_rows(q + static_cast<long long>(sub << g.pack) * g.d, g.q_stride, r0, w.len, g.d, g.pack, who);
-    sg.load_rows(d_out + static_cast<long long>(sub << g.pack) * g.d, g.out_stride, r0, w.len, g.d, g.pack, who);
+    Load::rows(tile, q + static_cast<long long>(sub << g.pack) * g.d, g.q_stride, r0, w.len, g.d, g.pack, part, lane);
+    Load::rows(tile + kTileElems, d_out + static_cast<long long>(sub << g.pack) * g.d, g.out_stride, r0, w.len, g.d, g.pack, part, lane);
+  };
+  const auto load_stats = [&](int it) {
     if (who < kRows) {
-      const int r = r0 + who;
+      const int sub = it / tiles, r = first_row + it % tiles * kRows + who;
       next_lse = kInf;  // (rows behind the last: probabilities of zero)
       next_delta = 0.f;
       if (r < rows) {
@@ -396,14 +425,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
       }
     }
   };
-  const auto store = [&](T* tile, float* stat, bool clean) {
-    if (clean) {
-      sq.template store<true>(tile, who);
-      sg.template store<true>(tile + kTileElems, who);
-    } else {
-      sq.template store<false>(tile, who);
-      sg.template store<false>(tile + kTileElems, who);
-    }
+  const auto store_stats = [&](float* stat) {
     if (who < kRows) {
       stat[who] = next_lse;
       stat[kRows + who] = next_delta;
@@ -415,11 +437,30 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
   // 32 rows from r0 on, rows b0.. of qt, gt and of the statistics
   const auto attend = [&](const T* qt, const T* gt, const float* lse_t, int b0, int r0) {
     const int first_tok = r0 >> g.pack;
+    typename Op::Frag q_rows[L::kSteps], g_rows[L::kSteps];
+#pragma unroll
+    for (int c = 0; c < L::kSteps; ++c) q_rows[c] = L::row_frag(qt, row_base, b0, c);
+#pragma unroll
+    for (int c = 0; c < L::kSteps; ++c) g_rows[c] = L::row_frag(gt, row_base, b0, c);
+    requested();
     floatx16_t s{}, dp{};
 #pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) Op::mma(s, L::row_frag(qt, row_base, b0, c), kf[c]);
+    for (int c = 0; c < L::kSteps; ++c) Op::mma(s, q_rows[c], kf[c]);
 #pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, L::row_frag(gt, row_base, b0, c), vf[c]);
+    for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, g_rows[c], vf[c]);
+    constexpr int kAhead = sizeof(T) == 2 ? L::kGroups : 1;
+    typename Op::Frag g_cols[kAhead][DP / 32], q_cols[kAhead][DP / 32];
+    const auto read_cols = [&](int c0) {
+#pragma unroll
+      for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+        for (int e = 0; e < DP / 32; ++e) {
+          g_cols[c][e] = L::col_frag(gt, col_base, b0, c0 + c, e);
+          q_cols[c][e] = L::col_frag(qt, col_base, b0, c0 + c, e);
+        }
+    };
+    read_cols(0);
+    requested();
     // register i: token first_tok + (i's part, the same for all lanes) + (4 half >> pack), head likewise
     const int apart = first_tok + ((4 * half) >> g.pack) - key;
     const int stride = BIAS ? table_stride(g) : 0;
@@ -443,11 +484,12 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
     }
 #pragma unroll
     for (int c = 0; c < L::kGroups; ++c) {
+      if (c != 0 && c % kAhead == 0) read_cols(c);
       const typename Op::Frag p = Op::from_acc(s, c), ds = Op::from_acc(dp, c);
 #pragma unroll
       for (int e = 0; e < DP / 32; ++e) {
-        Op::mma(dv[e], L::col_frag(gt, col_base, b0, c, e), p);
-        Op::mma(dk[e], L::col_frag(qt, col_base, b0, c, e), ds);
+        Op::mma(dv[e], g_cols[c % kAhead][e], p);
+        Op::mma(dk[e], q_cols[c % kAhead][e], ds);
       }
     }
   };
@@ -461,13 +503,25 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
       T* const mine = lds + wave * 2 * kTileElems;
       float* const stat = stats + wave * 2 * kRows;
       const auto range = [&](int first, int end) {
-        if (first + wave < end) load(first + wave);
+        if (first + wave < end) {
+          load(mine, first + wave);
+          load_stats(first + wave);
+        }
         for (int it = first + wave; it < end; it += kWaves) {
           wave_fence();
-          store(mine, stat, clean);
+          store_stats(stat);
+          landed<0>();
+          if (clean) {
+            Load::clean(mine, 0, lane);
+            Load::clean(mine + kTileElems, 0, lane);
+          }
           wave_fence();
-          if (it + kWaves < end) load(it + kWaves);
           attend(mine, mine + kTileElems, stat, 0, first_row + it % tiles * kRows);
+          lds_done();
+          if (it + kWaves < end) {
+            load(mine, it + kWaves);
+            load_stats(it + kWaves);
+          }
         }
       };
       if (BIAS) {
@@ -492,18 +546,27 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
       __syncthreads();
       join_parts<DP>(parts, kPart, wave, lane, joined_k);
     } else {
-      load(0);
+      load(lds, 0);
+      load_stats(0);
       for (int it = 0; it < steps; ++it) {
         T* const tile = lds + (it & 1) * 2 * kTileElems;
         float* const stat = stats + (it & 1) * 2 * kRows;
-        store(tile, stat, clean);
+        store_stats(stat);
+        landed<0>();
+        if (clean) {
+          Load::clean(tile, part, lane);
+          Load::clean(tile + kTileElems, part, lane);
+        }
         const int sub = it / tiles, r0 = first_row + it % tiles * kRows;
         if (BIAS && it % tiles == 0) {
           __syncthreads();  // (the last tile of the heads before is done with their bias)
           fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
         }
         __syncthreads();
-        if (it + 1 < steps) load(it + 1);
+        if (it + 1 < steps) {
+          load(lds + (~it & 1) * 2 * kTileElems, it + 1);
+          load_stats(it + 1);
+        }
 #pragma unroll
         for (int b = 0; b < kRows / 32; ++b)
           if ((r0 + 32 * b + 31) >> g.pack >= key0) attend(tile, tile + kTileElems, stat, 32 * b, r0 + 32 * b);

@@ -86,22 +86,16 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
   if (SPLIT && BIAS) __syncthreads();
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
-  const int who = SPLIT ? lane : static_cast<int>(threadIdx.x);
-  Stage<T, DP, kKeys, kTogether> sk, sv;
+  typedef Stage<T, DP, kKeys, kTogether> Load;
+  const int part = SPLIT ? 0 : wave;  // of a tile's load
   floatx16_t o[DP / 32];
   float m, total;
-  const auto load = [&](int t) {
-    sk.load_keys(k, g.k_stride, t * kKeys, w.len, g.d, who);
-    sv.load_keys(v, g.v_stride, t * kKeys, w.len, g.d, who);
-  };
-  const auto store = [&](T* tile, bool clean) {
-    sk.template store<false>(tile, who);
-    if (clean) sv.template store<true>(tile + kTileElems, who);
-    else sv.template store<false>(tile + kTileElems, who);
-  };
+  const auto load_k = [&](T* tile, int t) { Load::keys(tile, k, g.k_stride, t * kKeys, w.len, g.d, part, lane); };
+  const auto load_v = [&](T* tile, int t) { Load::keys(tile, v, g.v_stride, t * kKeys, w.len, g.d, part, lane); };
   const uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
-  // the keys from key0 on, at kt and vt, for this wavefront's rows
-  const auto attend = [&](const T* kt, const T* vt, int key0) {
+  // The keys from key0 on, at kt and vt, for this wavefront's rows.  k_read() is called when K's tile has been read, v_there()
+  // before V's is.
+  const auto attend = [&](const T* kt, const T* vt, int key0, auto&& k_read, auto&& v_there) {
     typename Op::Frag rows[2][L::kSteps];
     const auto read_rows = [&](int b) {
 #pragma unroll
@@ -126,6 +120,8 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
 #pragma unroll
         for (int e = 0; e < DP / 32; ++e) vf[c][e] = L::col_frag(vt, col_base, 32 * b, c0 + c, e);
     };
+    k_read();
+    v_there();
     read_values(0, 0);
     requested();
     float top = -kInf;
@@ -208,29 +204,48 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
     m = -kInf;       // maximum of the logits so far, times log2 e
     total = 0.f;     // this half's share of the sum
     if constexpr (SPLIT) {
-      T* const mine = lds + wave * 2 * kTileElems;
+      // one tile of each: K's next one is requested when the scores are there, V's at the end
+      T* const kt = lds + wave * 2 * kTileElems;
+      T* const vt = kt + kTileElems;
       const int tiles = last_tok / kKeys + 1;
-      if (wave < tiles) load(wave);
+      if (wave < tiles) {
+        load_k(kt, wave);
+        load_v(vt, wave);
+      }
       for (int t = wave; t < tiles; t += kWaves) {
-        wave_fence();
-        store(mine, clean);
-        wave_fence();
-        if (t + kWaves < tiles) load(t + kWaves);
-        attend(mine, mine + kTileElems, t * kKeys);
+        const bool more = t + kWaves < tiles;
+        landed<Load::kLoads>();
+        attend(kt, vt, t * kKeys,
+               [&] {
+                 lds_done();
+                 if (more) load_k(kt, t + kWaves);
+               },
+               [&] {
+                 if (more) landed<Load::kLoads>();
+                 else landed<0>();
+                 if (clean) Load::clean(vt, 0, lane);
+               });
+        lds_done();
+        if (more) load_v(vt, t + kWaves);
       }
     } else {
       const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);  // of the workgroup: the keys it sees
       const int tiles = (end_tok + kKeys - 1) / kKeys;
-      load(0);
+      load_k(lds, 0);
+      load_v(lds + kTileElems, 0);
       for (int t = 0; t < tiles; ++t) {
         T* const tile = lds + (t & 1) * 2 * kTileElems;
-        store(tile, clean);
+        landed<0>();
+        if (clean) Load::clean(tile + kTileElems, part, lane);
         __syncthreads();
-        if (t + 1 < tiles) load(t + 1);
-        if (t * kKeys <= last_tok) attend(tile, tile + kTileElems, t * kKeys);
+        if (t + 1 < tiles) {
+          T* const next = lds + (~t & 1) * 2 * kTileElems;
+          load_k(next, t + 1);
+          load_v(next + kTileElems, t + 1);
+        }
+        if (t * kKeys <= last_tok) attend(tile, tile + kTileElems, t * kKeys, [] {}, [] {});
       }
     }
-
     total = sum_of_halves(total);
     if constexpr (SPLIT) {
       if (half == 0) {
