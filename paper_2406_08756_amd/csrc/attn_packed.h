@@ -38,8 +38,12 @@ __device__ __forceinline__ float max_of_halves(float v) {
   const float2 b = of_both_halves(v);
   return fmaxf(b.x, b.y);
 }
-// What is requested above is requested before anything below is done.
-__device__ __forceinline__ void requested() { __builtin_amdgcn_sched_barrier(0); }
+// What the compiler has derived from x is derived again.
+__device__ __forceinline__ void forget(uint32_t& x) { asm volatile("" : "+v"(x)); }
+// x is computed before this point, not where it is used.
+template <typename X> __device__ __forceinline__ void stay(X& x) { asm volatile("" : "+v"(x)); }
+// What stands above is issued before anything below.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < kInf; }
 
@@ -102,6 +106,62 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int til
   return true;
 }
 
+// The same, the tiles with the most to see first over all sequences: a tile's size is its number, counted from the end that
+// sees least (rows: the start, keys: the end), and slot 0 is one of the largest.  The card waits for the last workgroup, and in
+// the order of the sequences that may be a large one (four sequences of 2048 tokens: 1.4 times the work's share).  For up to
+// 128 sequences; with more there are many tiles of every size and the plain order serves.
+constexpr int kRankedSequences = 128;
+__device__ __forceinline__ bool find_ranked_tile(const PackedAttn& g, int slot, int tile_log, int pack, SeqTile* out) {
+  if (g.sequences > kRankedSequences) return find_tile<true>(g, slot, tile_log, pack, out);
+  const int lane = threadIdx.x & (kWave - 1);
+  int tiles[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = k * kWave + lane;
+    tiles[k] = s < g.sequences ? ((sequence_span(g, s).y << pack) + (1 << tile_log) - 1) >> tile_log : 0;
+  }
+  // how many tiles have a number of `from` or more: falls with `from`; each lane counts for one number
+  const auto count = [&](int from) {
+    int sum = 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      for (int i = 0; i < min(g.sequences - k * kWave, kWave); ++i) sum += max(__builtin_amdgcn_readlane(tiles[k], i) - from, 0);
+    return sum;
+  };
+  // the largest number of which, with those above it, there are more than `slot`: in [lo, lo + range)
+  int lo = 0, range = (g.tokens << pack >> tile_log) + 1, above = 0;
+  while (true) {
+    const int step = (range + kWave - 1) / kWave, from = lo + lane * step;
+    const int n = count(from);
+    const unsigned long long more = __ballot(n > slot);
+    if (more == 0) return false;
+    const int last = 63 - __builtin_clzll(more);
+    if (step == 1) {
+      above = last < kWave - 1 ? __builtin_amdgcn_readlane(n, last + 1) : __builtin_amdgcn_readfirstlane(count(lo + kWave));
+      lo += last;
+      break;
+    }
+    lo += last * step;
+    range = step;
+  }
+  int rank = slot - above, at = 0;  // among the sequences that have a tile of that number
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    unsigned long long has = __ballot(tiles[k] > lo);
+    const int n = __builtin_popcountll(has);
+    if (rank >= 0 && rank < n) {
+      for (int i = 0; i < rank; ++i) has &= has - 1;
+      at = k * kWave + __builtin_ctzll(has);
+    }
+    rank -= n;
+  }
+  const int2 span = sequence_span(g, at);
+  out->start = __builtin_amdgcn_readfirstlane(span.x);
+  out->len = __builtin_amdgcn_readfirstlane(span.y);
+  out->tile = lo;
+  return true;
+}
+
 // ---- operands ---------------------------------------------------------------
 template <typename T> struct Operand;
 template <> struct Operand<bf16_t> {
@@ -144,6 +204,27 @@ template <> struct Operand<float> {
     return s;
   }
 };
+
+// acc += A B in an accumulation register.  A kernel of one wavefront per SIMD has 256 of them beside 256 ordinary ones, and
+// sums that live through its branches were copied back and forth between the two kinds (272 moves per block of 32 rows)
+// until their kind was named.  What the compiler does for its own instructions stands here: two wait states behind a vector
+// instruction that wrote A or B, and settled() before the sums are read.
+__device__ __forceinline__ void mma_aside(floatx16_t& acc, bf16x8_t a, bf16x8_t b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+#endif
+}
+__device__ __forceinline__ void mma_aside(floatx16_t& acc, floatx4_t a, floatx4_t b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+  for (int j = 0; j < 4; ++j) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x2_f32 %0, %1, %2, %0" : "+a"(acc) : "v"(a[j]), "v"(b[j]));
+#endif
+}
+__device__ __forceinline__ void settled(floatx16_t& acc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc));
+#endif
+}
 
 // 16 bytes with every infinity and NaN replaced by zero.
 __device__ __forceinline__ uintx4_t without_nonfinite(uintx4_t w, const bf16_t*) {

@@ -4,6 +4,8 @@
 //   keys:  dV = P^T d_out and dK = scale dS^T Q, over all rows of all heads of the group that see the key
 // Each result is summed by one workgroup in one order: no atomics between workgroups, the same bits every time.  The price is
 // that both kernels form the scores and d_out V^T: seven products instead of five.
+#include <type_traits>
+
 #include "attn_packed.h"
 
 namespace lynx {
@@ -16,11 +18,13 @@ constexpr int kBlockStride = 33, kBlockPad = 32, kBlockFloats = 32 * kBlockStrid
 __host__ __device__ __forceinline__ int distances(const PackedAttn& g) { return g.far + 64; }
 __host__ __device__ __forceinline__ int by_distance_floats(const PackedAttn& g) { return (distances(g) << g.pack) + kBlockFloats; }  // of a wavefront
 
-// Two tiles, two of each, or one of each wavefront.
+// K and V in tiles of 32 keys: four of each, which leaves a tile the time of two to arrive, or three and two where the sums of
+// the bias's gradient or fp32 leave no room for more beside another workgroup; or one of each wavefront.
 template <typename T, int DP, bool BIAS, bool SPLIT> struct Rows {
-  static constexpr int kKeys = sizeof(T) == 2 && !BIAS && !SPLIT ? 64 : 32;
-  static constexpr int kTileElems = kKeys * DP;
-  static constexpr size_t kTiles = (SPLIT ? 2 * kWaves : 4) * static_cast<size_t>(kTileElems) * sizeof(T);
+  static constexpr int kTileElems = 32 * DP;
+  static constexpr bool kFew = BIAS || sizeof(T) * DP == 512;
+  static constexpr int kTileCount = SPLIT ? 2 * kWaves : kFew ? 5 : 8;
+  static constexpr size_t kTiles = kTileCount * static_cast<size_t>(kTileElems) * sizeof(T);
   static constexpr size_t kLds = kTiles + (SPLIT ? kWaves * sizeof(uint32_t) : 0);
 };
 template <typename T, int DP, bool SPLIT> struct Keys {
@@ -68,7 +72,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
   typedef Rows<T, DP, BIAS, SPLIT> S;
-  constexpr int kKeys = S::kKeys, kTileElems = S::kTileElems, kRowsLog = rows_log(SPLIT);
+  constexpr int kTileElems = S::kTileElems, kRowsLog = rows_log(SPLIT);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   T* const lds = reinterpret_cast<T*>(smem_raw);
   float* const bias = reinterpret_cast<float*>(smem_raw + S::kLds);
@@ -80,7 +84,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int heads = 1 << g.pack;
   SeqTile w;
-  if (!find_tile</*LAST_FIRST=*/true>(g, slot, kRowsLog, g.pack, &w)) {
+  if (!(SPLIT ? find_tile</*LAST_FIRST=*/true>(g, slot, kRowsLog, g.pack, &w) : find_ranked_tile(g, slot, kRowsLog, g.pack, &w))) {
     if (BIAS)
       for (int x = threadIdx.x; x < heads * g.buckets; x += kThreads)
         g.partials[(static_cast<long long>(slot) * g.heads + head0) * g.buckets + x] = 0.f;
@@ -124,7 +128,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
     if (there) {
       const long long stat = static_cast<long long>(head0 + hp) * g.tokens + w.start + tok;
       lse2 = offset2(g.lse[stat]);
-      if (half == 0 && (!SPLIT || wave == 0)) g.delta[stat] = delta;
     }
   }
   const float* const my_bias = BIAS ? bias + hp * table_stride(g) + kPad : nullptr;
@@ -133,85 +136,159 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   if (SPLIT && BIAS) __syncthreads();
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
-  typedef Stage<T, DP, kKeys, kTogether> Load;
+  typedef Stage<T, DP, 32, kTogether> Load;
   const int part = SPLIT ? 0 : wave;  // of a tile's load
   floatx16_t acc[DP / 32];
-  const auto load_k = [&](T* tile, int t) { Load::keys(tile, k, g.k_stride, t * kKeys, w.len, g.d, part, lane); };
-  const auto load_v = [&](T* tile, int t) { Load::keys(tile, v, g.v_stride, t * kKeys, w.len, g.d, part, lane); };
-  const uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
-  // 32 keys from key0 on, rows b0.. of kt and vt.  v_read() is called when V's have been read.
-  const auto attend = [&](const T* kt, const T* vt, int b0, int key0, bool clean, auto&& v_read) {
-    typename Op::Frag k_rows[L::kSteps], v_rows[L::kSteps];
+  const auto load_k = [&](T* tile, int t) { Load::keys(tile, k, g.k_stride, 32 * t, w.len, g.d, part, lane); };
+  const auto load_v = [&](T* tile, int t) { Load::keys(tile, v, g.v_stride, 32 * t, w.len, g.d, part, lane); };
+  uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
+  // A tile goes by in three passes of matrix instructions, with the arithmetic between them: d_out V^T, and the probabilities;
+  // the next tile's scores, and ds; the sum over K.  The order is written out (in_order()), with fragments kRing steps ahead
+  // of their use: left to itself the compiler keeps one and waits for each.
+  constexpr int kRing = 4, kSumSteps = L::kGroups * (DP / 32), kFrags = 2 * L::kSteps + kSumSteps;
+  typename Op::Frag ring[kRing];
+  // the fragments of the three passes: of V, of the next tile's K, of K
+  const auto frag = [&](const T* kt, const T* vt, const T* next_kt, int i) {
+    if (i < L::kSteps) return L::row_frag(vt, row_base, 0, i);
+    if (i < 2 * L::kSteps) return L::row_frag(next_kt, row_base, 0, i - L::kSteps);
+    const int j = i - 2 * L::kSteps;
+    return L::col_frag(kt, col_base, 0, j / (DP / 32), j % (DP / 32));
+  };
+  const auto first_frags = [&](const T* kt, const T* vt, const T* next_kt, int first) {
+    forget(row_base);  // (the offsets of all fragments, kept, would be 16 registers)
+    forget(col_base);
 #pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) k_rows[c] = L::row_frag(kt, row_base, b0, c);
+    for (int i = 0; i < kRing; ++i) ring[i] = frag(kt, vt, next_kt, first + i);
+    in_order();
+  };
+  const auto form_scores = [&](const T* kt, floatx16_t& s) {
+    first_frags(kt, kt, kt, L::kSteps);
+    s = floatx16_t{};
 #pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) v_rows[c] = L::row_frag(vt, row_base, b0, c);
-    requested();
-    floatx16_t s{}, dp{};
-#pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) Op::mma(s, k_rows[c], qf[c]);
-#pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, v_rows[c], gf[c]);
-    v_read();
-    constexpr int kAhead = sizeof(T) == 2 ? L::kGroups : 1;
-    typename Op::Frag k_cols[kAhead][DP / 32];
-    const auto read_cols = [&](int c0) {
-#pragma unroll
-      for (int c = 0; c < kAhead; ++c)
-#pragma unroll
-        for (int e = 0; e < DP / 32; ++e) k_cols[c][e] = L::col_frag(kt, col_base, b0, c0 + c, e);
-    };
-    read_cols(0);
-    requested();
-    const int apart = tok - key0 - 4 * half;
-    const bool near = BIAS && first_tok - (key0 + 31) < g.far, edge = key0 + 31 > first_tok;
-    const float offset = BIAS && !near ? lse2 - my_bias[g.far] : lse2;
-    if (BIAS && near) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale2, my_bias[apart - acc_row(i, 0)] - lse2);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale2, -offset);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = exp2_fast(s[i]) * (dp[i] - delta);
-    if (edge) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (apart < acc_row(i, 0)) s[i] = 0.f;
-    }
-    if (!there) s = floatx16_t{};
-    if (BIAS && !clean) {
-      if (near) {
-        float* const block = my_sums + (distances(g) << g.pack) + kBlockPad;
-        wave_fence();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) block[(lane & 31) * kBlockStride + acc_row(i, half)] = s[i];
-        wave_fence();
-        // lane: the diagonal token - key = lane - 31, of each head in turn
-        const int diagonal = lane - 31, distance = first_tok - key0 + diagonal, tokens = 32 >> g.pack;
-        for (int h = 0; h < heads; ++h) {
-          float sum = 0.f;
-#pragma unroll 8
-          for (int r = 0; r < tokens; ++r) {
-            const float x = block[((r << g.pack) + h) * kBlockStride + r - diagonal];
-            sum += r - diagonal >= 0 && r - diagonal < 32 ? x : 0.f;
-          }
-          if (distance >= 0 && diagonal < tokens) my_sums[h * distances(g) + distance] += sum;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) far_sum += s[i];
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < L::kGroups; ++c) {
-      if (c != 0 && c % kAhead == 0) read_cols(c);
-      const typename Op::Frag ds = Op::from_acc(s, c);
-#pragma unroll
-      for (int e = 0; e < DP / 32; ++e) Op::mma(acc[e], k_cols[c % kAhead][e], ds);
+    for (int i = 0; i < L::kSteps; ++i) {
+      Op::mma(s, ring[i % kRing], qf[i]);
+      if (i + kRing < L::kSteps) ring[i % kRing] = frag(kt, kt, kt, L::kSteps + i + kRing);
+      in_order();
     }
   };
+  // scores to exponents, with a bias (without one the probabilities do it), of the keys from key0 on
+  const auto exponents = [&](floatx16_t& s, int key0) {
+    if (!BIAS) return;
+    const int apart = tok - key0 - 4 * half;
+    if (first_tok - (key0 + 31) < g.far) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], scale2, my_bias[apart - acc_row(e, 0)] - lse2);
+    } else {
+      const float offset = my_bias[g.far] - lse2;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], scale2, offset);
+    }
+  };
+  const auto probability = [&](float s) { return exp2_fast(BIAS ? s : __builtin_fmaf(s, scale2, -lse2)); };
+  // The bias's share of ds, of the keys from key0 on.
+  const auto add_to_table = [&](const floatx16_t& ds, int key0) {
+    if (first_tok - (key0 + 31) >= g.far) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) far_sum += ds[e];
+      return;
+    }
+    float* const block = my_sums + (distances(g) << g.pack) + kBlockPad;
+    wave_fence();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) block[(lane & 31) * kBlockStride + acc_row(e, half)] = ds[e];
+    wave_fence();
+    // lane: the diagonal token - key = lane - 31, of each head in turn
+    const int diagonal = lane - 31, distance = first_tok - key0 + diagonal, tokens = 32 >> g.pack;
+    for (int h = 0; h < heads; ++h) {
+      float sum = 0.f;
+#pragma unroll 8
+      for (int r = 0; r < tokens; ++r) {
+        const float x = block[((r << g.pack) + h) * kBlockStride + r - diagonal];
+        sum += r - diagonal >= 0 && r - diagonal < 32 ? x : 0.f;
+      }
+      if (distance >= 0 && diagonal < tokens) my_sums[h * distances(g) + distance] += sum;
+    }
+  };
+  // s: the exponents of the tile at kt (scores without a bias); next_kt: the next tile, of which it leaves them in `next`.
+  const auto attend = [&](const T* kt, const T* vt, const T* next_kt, floatx16_t& s, floatx16_t& next, int key0, bool clean, auto has_next) {
+    constexpr bool NEXT = decltype(has_next)::value;
+    first_frags(kt, vt, next_kt, 0);
+    const auto turn = [&](int i) {  // the i-th of the fragments that are used has been: without a next tile its own are left out
+      const int n = NEXT || i + kRing < L::kSteps ? i + kRing : i + kRing + L::kSteps;
+      if (n < kFrags) ring[i % kRing] = frag(kt, vt, next_kt, n);
+    };
+    floatx16_t dp{};
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i) {
+      Op::mma(dp, ring[i % kRing], gf[i]);
+      turn(i);
+#pragma unroll
+      for (int e = i * 16 / L::kSteps; e < (i + 1) * 16 / L::kSteps; ++e) {
+        float p = probability(s[e]);
+        stay(p);
+        s[e] = p;
+      }
+      in_order();
+    }
+    if (NEXT) next = floatx16_t{};
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i) {
+      if (NEXT) {
+        Op::mma(next, ring[i % kRing], qf[i]);
+        turn(L::kSteps + i);
+      }
+#pragma unroll
+      for (int e = i * 16 / L::kSteps; e < (i + 1) * 16 / L::kSteps; ++e) {
+        float ds = s[e] * (dp[e] - delta);
+        if (NEXT) stay(ds);
+        s[e] = ds;
+      }
+      if (NEXT) in_order();
+    }
+    if (key0 + 31 > first_tok || !there) {  // (by a choice: what is masked may be NaN)
+      const int apart = there ? tok - key0 - 4 * half : -1;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (apart < acc_row(e, 0)) s[e] = 0.f;
+    }
+    if (BIAS && !clean) add_to_table(s, key0);
+    if (NEXT) exponents(next, key0 + (SPLIT ? 0 : 32));
+#pragma unroll
+    for (int i = 0; i < kSumSteps; ++i) {
+      const typename Op::Frag ds = Op::from_acc(s, i / (DP / 32));
+      Op::mma(acc[i % (DP / 32)], ring[i % kRing], ds);
+      turn((NEXT ? 2 : 1) * L::kSteps + i);
+      in_order();
+    }
+  };
+  // Where all keys of these rows are in one tile, delta comes from the probabilities instead: with so few the rounding of `out`
+  // is felt, and a row that sees one key has a ds of zero.
+  const auto own_delta = [&](const T* vt, const floatx16_t& s) {
+    first_frags(vt, vt, vt, 0);
+    floatx16_t dp{};
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i) {
+      Op::mma(dp, ring[i % kRing], gf[i]);
+      if (i + kRing < L::kSteps) ring[i % kRing] = frag(vt, vt, vt, i + kRing);
+    }
+    const int apart = tok - 4 * half;
+    float sum = 0.f, weight = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float p = probability(s[e]);
+      sum += apart < acc_row(e, 0) ? 0.f : p * dp[e];
+      weight += apart < acc_row(e, 0) ? 0.f : p;
+    }
+    sum = sum_of_halves(sum);
+    weight = sum_of_halves(weight);
+    delta = weight == 0.f ? 0.f : sum / weight;
+  };
+  const bool one_tile = last_tok >= 0 && last_tok < 32;
+  const auto write_delta = [&] {
+    if (there && half == 0 && (!SPLIT || wave == 0)) g.delta[static_cast<long long>(head0 + hp) * g.tokens + w.start + tok] = delta;
+  };
+  constexpr std::true_type yes;
+  constexpr std::false_type no;
 
   bool spoilt = false;
   float joined[DP / 8];  // SPLIT: this lane's columns of its row
@@ -219,25 +296,25 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) acc[b] = floatx16_t{};
     if constexpr (SPLIT) {
-      // one tile of each: V's next one is requested when it has been read, K's at the end
       T* const kt = lds + wave * 2 * kTileElems;
-      T* const vt = kt + kTileElems;
-      const int tiles = last_tok / kKeys + 1;
-      if (wave < tiles) {
-        load_v(vt, wave);
-        load_k(kt, wave);
-      }
+      const int tiles = last_tok / 32 + 1;
+      const auto load = [&](int t) {
+        load_k(kt, t);
+        load_v(kt + kTileElems, t);
+      };
+      if (wave < tiles) load(wave);
       for (int t = wave; t < tiles; t += kWaves) {
-        const bool more = t + kWaves < tiles;
         landed<0>();
         if (clean) Load::clean(kt, 0, lane);
-        attend(kt, vt, 0, t * kKeys, clean, [&] {
-          lds_done();
-          if (more) load_v(vt, t + kWaves);
-        });
+        floatx16_t s;
+        form_scores(kt, s);
+        exponents(s, 32 * t);
+        if (one_tile && !clean) own_delta(kt + kTileElems, s);
+        attend(kt, kt + kTileElems, kt, s, s, 32 * t, clean, no);
         lds_done();
-        if (more) load_k(kt, t + kWaves);
+        if (t + kWaves < tiles) load(t + kWaves);
       }
+      if (!clean) write_delta();
       __syncthreads();
       float* const parts = reinterpret_cast<float*>(smem_raw);
       constexpr size_t kPart = 2 * kTileElems * sizeof(T) / sizeof(float);
@@ -247,23 +324,42 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
       join_parts<DP>(parts, kPart, wave, lane, joined);
     } else {
       const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);
-      const int tiles = (end_tok + kKeys - 1) / kKeys;
-      load_k(lds, 0);
-      load_v(lds + kTileElems, 0);
-      for (int t = 0; t < tiles; ++t) {
-        T* const tile = lds + (t & 1) * 2 * kTileElems;
-        landed<0>();
-        if (clean) Load::clean(tile, part, lane);
+      const int tiles = (end_tok + 31) / 32;
+      constexpr int kKs = S::kFew ? 3 : 4, kVs = S::kFew ? 2 : 4;
+      const auto k_tile = [&](int t) { return lds + t % kKs * kTileElems; };
+      const auto v_tile = [&](int t) { return lds + (kKs + t % kVs) * kTileElems; };
+      const auto load = [&](int kt, int vt) {
+        if (kt < tiles) load_k(k_tile(kt), kt);
+        if (vt < tiles) load_v(v_tile(vt), vt);
+      };
+      // K up to tile t and V up to the one before are there, for all wavefronts, and the tiles before t - 1 have been read:
+      // their place takes others.
+      const auto arrive = [&](int t) {
+        if (!S::kFew && t + 1 < tiles) landed<2 * Load::kLoads>();
+        else landed<0>();
+        if (clean && t < tiles) Load::clean(k_tile(t), part, lane);
         __syncthreads();
-        if (t + 1 < tiles) {
-          T* const next = lds + (~t & 1) * 2 * kTileElems;
-          load_k(next, t + 1);
-          load_v(next + kTileElems, t + 1);
-        }
-#pragma unroll
-        for (int b = 0; b < kKeys / 32; ++b)
-          if (t * kKeys + 32 * b <= last_tok) attend(tile, tile + kTileElems, 32 * b, t * kKeys + 32 * b, clean, [] {});
+        if (S::kFew) load(t + 1, t == 0 ? tiles : t);  // (the first V has been asked for)
+        else load(t + 2, t + 2);
+      };
+      load(0, 0);
+      if (!S::kFew) load(1, 1);
+      arrive(0);
+      floatx16_t s, next;
+      form_scores(k_tile(0), s);
+      exponents(s, 0);
+      if (!clean) {
+        if (one_tile) own_delta(v_tile(0), s);
+        write_delta();
       }
+      int t = 0;
+      for (; t + 1 < tiles; ++t) {
+        arrive(t + 1);
+        attend(k_tile(t), v_tile(t), k_tile(t + 1), s, next, 32 * t, clean, yes);
+        s = next;
+      }
+      if (S::kFew && t > 0) arrive(tiles);
+      attend(k_tile(t), v_tile(t), k_tile(t), s, s, 32 * t, clean, no);
     }
     if (clean) break;
     float check = 0.f;
@@ -442,7 +538,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
     for (int c = 0; c < L::kSteps; ++c) q_rows[c] = L::row_frag(qt, row_base, b0, c);
 #pragma unroll
     for (int c = 0; c < L::kSteps; ++c) g_rows[c] = L::row_frag(gt, row_base, b0, c);
-    requested();
+    in_order();
     floatx16_t s{}, dp{};
 #pragma unroll
     for (int c = 0; c < L::kSteps; ++c) Op::mma(s, q_rows[c], kf[c]);
@@ -460,7 +556,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
         }
     };
     read_cols(0);
-    requested();
+    in_order();
     // register i: token first_tok + (i's part, the same for all lanes) + (4 half >> pack), head likewise
     const int apart = first_tok + ((4 * half) >> g.pack) - key;
     const int stride = BIAS ? table_stride(g) : 0;

@@ -1,15 +1,16 @@
 // Causal attention over packed sequences with grouped heads, forward: out = softmax(scale Q K^T + bias) V, one pass over the
 // keys with a running maximum and sum; no seq x seq tensor.
+#include <type_traits>
+
 #include "attn_packed.h"
 
 namespace lynx {
 namespace {
 
+// K and V in tiles of 32 keys, kCopies of each; or one of each wavefront.
 template <typename T, int DP, bool SPLIT> struct Fwd {
-  static constexpr int kKeys = sizeof(T) == 2 && !SPLIT ? 64 : 32;  // keys per tile
-  static constexpr int kTileElems = kKeys * DP;
-  // K and V, two of each, or one of each wavefront
-  static constexpr size_t kTiles = (SPLIT ? 2 * kWaves : 4) * static_cast<size_t>(kTileElems) * sizeof(T);
+  static constexpr int kTileElems = 32 * DP, kCopies = SPLIT ? kWaves : sizeof(T) * DP == 512 ? 3 : 4;
+  static constexpr size_t kTiles = 2 * kCopies * static_cast<size_t>(kTileElems) * sizeof(T);
   static constexpr size_t kLds = kTiles + (SPLIT ? 2 * kWaves * 32 * sizeof(float) : 0);
 };
 
@@ -48,16 +49,17 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
   typedef Fwd<T, DP, SPLIT> S;
-  constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32, kTileElems = S::kTileElems, kRowsLog = rows_log(SPLIT);
+  constexpr int kTileElems = S::kTileElems, kRowsLog = rows_log(SPLIT);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   T* const lds = reinterpret_cast<T*>(smem_raw);
-  float* const tops = reinterpret_cast<float*>(smem_raw + S::kTiles);  // SPLIT: each wavefront's maxima and sums
+  float* const tops = reinterpret_cast<float*>(smem_raw + S::kTiles);  // SPLIT: each wavefront's maxima, then sums
   float* const bias = reinterpret_cast<float*>(smem_raw + S::kLds);
 
   const int subs = g.heads >> g.pack;
   const int head0 = (static_cast<int>(blockIdx.x) % subs) << g.pack;
   SeqTile w;
-  if (!find_tile</*LAST_FIRST=*/true>(g, static_cast<int>(blockIdx.x) / subs, kRowsLog, g.pack, &w)) return;
+  const int slot = static_cast<int>(blockIdx.x) / subs;
+  if (!(SPLIT ? find_tile</*LAST_FIRST=*/true>(g, slot, kRowsLog, g.pack, &w) : find_ranked_tile(g, slot, kRowsLog, g.pack, &w))) return;
   if (BIAS) fill_bias<T, kThreads>(g, head0, bias);
 
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
@@ -86,88 +88,54 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
   if (SPLIT && BIAS) __syncthreads();
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
-  typedef Stage<T, DP, kKeys, kTogether> Load;
+  typedef Stage<T, DP, 32, kTogether> Load;
   const int part = SPLIT ? 0 : wave;  // of a tile's load
   floatx16_t o[DP / 32];
   float m, total;
-  const auto load_k = [&](T* tile, int t) { Load::keys(tile, k, g.k_stride, t * kKeys, w.len, g.d, part, lane); };
-  const auto load_v = [&](T* tile, int t) { Load::keys(tile, v, g.v_stride, t * kKeys, w.len, g.d, part, lane); };
-  const uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
-  // The keys from key0 on, at kt and vt, for this wavefront's rows.  k_read() is called when K's tile has been read, v_there()
-  // before V's is.
-  const auto attend = [&](const T* kt, const T* vt, int key0, auto&& k_read, auto&& v_there) {
-    typename Op::Frag rows[2][L::kSteps];
-    const auto read_rows = [&](int b) {
+  const auto load_k = [&](T* tile, int t) { Load::keys(tile, k, g.k_stride, 32 * t, w.len, g.d, part, lane); };
+  const auto load_v = [&](T* tile, int t) { Load::keys(tile, v, g.v_stride, 32 * t, w.len, g.d, part, lane); };
+  uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
+  // A tile goes by in two passes of matrix instructions, with the arithmetic between them: the scores of tile t + 1, and the
+  // probabilities of tile t; the sum of tile t over V, and the maxima of tile t + 1.  The order is written out (in_order()), with
+  // fragments kRing steps ahead of their use: left to itself the compiler keeps one and waits for each.
+  constexpr int kRing = 4, kValueSteps = L::kGroups * (DP / 32);
+  typename Op::Frag ring[kRing];
+  // the fragments of a tile's two passes: of K (kt), then of V (vt)
+  const auto frag = [&](const T* kt, const T* vt, int i) {
+    if (i < L::kSteps) return L::row_frag(kt, row_base, 0, i);
+    const int j = i - L::kSteps;
+    return L::col_frag(vt, col_base, 0, j / (DP / 32), j % (DP / 32));
+  };
+  const auto first_frags = [&](const T* kt, const T* vt, int first) {
+    forget(row_base);  // (the offsets of all fragments, kept, would be 16 registers)
+    forget(col_base);
 #pragma unroll
-      for (int c = 0; c < L::kSteps; ++c) rows[b & 1][c] = L::row_frag(kt, row_base, 32 * b, c);
-    };
-    floatx16_t s[kBlocks];
-    read_rows(0);
-    requested();
+    for (int i = 0; i < kRing; ++i) ring[i] = frag(kt, vt, first + i);
+    in_order();
+  };
+  // scores to logits (without a bias unscaled: the probabilities scale them) of the keys from key0 on
+  const auto logits = [&](floatx16_t& s, int key0) {
+    const int apart = tok - key0 - 4 * half;
+    if (BIAS && first_tok - (key0 + 31) < g.far) {
+      const float* const at = my_bias + apart;
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-      if (b + 1 < kBlocks) read_rows(b + 1);
-      s[b] = floatx16_t{};
+      for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], scale2, at[-acc_row(e, 0)]);
+    } else if (BIAS) {
+      const float far = my_bias[g.far];
 #pragma unroll
-      for (int c = 0; c < L::kSteps; ++c) Op::mma(s[b], rows[b & 1][c], qf[c]);
+      for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], scale2, far);
     }
-    // V's fragments are requested ahead of the arithmetic that its products wait for, as many as registers are free
-    constexpr int kAhead = sizeof(T) == 2 ? L::kGroups : 1;
-    typename Op::Frag vf[kAhead][DP / 32];
-    const auto read_values = [&](int b, int c0) {
+    if (key0 + 31 > first_tok) {  // (by a choice, not a sum: a masked score may be NaN)
 #pragma unroll
-      for (int c = 0; c < kAhead; ++c)
-#pragma unroll
-        for (int e = 0; e < DP / 32; ++e) vf[c][e] = L::col_frag(vt, col_base, 32 * b, c0 + c, e);
-    };
-    k_read();
-    v_there();
-    read_values(0, 0);
-    requested();
-    float top = -kInf;
-    const bool edge = key0 + kKeys - 1 > first_tok;
-    if (BIAS) {
-      const int apart = tok - key0 - 4 * half;
-      if (first_tok - (key0 + kKeys - 1) < g.far) {
-        const float* const at = my_bias + apart;
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            // (masked by a choice: the sum would be NaN where the score is)
-            const float z = __builtin_fmaf(s[b][i], scale2, at[-(32 * b + acc_row(i, 0))]);
-            s[b][i] = apart >= 32 * b + acc_row(i, 0) ? z : -kInf;
-            top = fmaxf(top, s[b][i]);
-          }
-      } else {
-        const float far = my_bias[g.far];
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            s[b][i] = __builtin_fmaf(s[b][i], scale2, far);
-            top = fmaxf(top, s[b][i]);
-          }
-      }
-    } else {
-      if (edge) {
-        const int apart = tok - key0 - 4 * half;
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (apart < 32 * b + acc_row(i, 0)) s[b][i] = -kInf;
-      }
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-      top *= scale2;
+      for (int e = 0; e < 16; ++e)
+        if (apart < acc_row(e, 0)) s[e] = -kInf;
     }
-    top = max_of_halves(top);
-    // The reference follows the maximum only where that has left it 2^8 behind: probabilities up to 256 lose nothing in
-    // fp32 sums or by a rounding to the storage type, and the accumulators are hardly ever scaled.  A row decides for itself:
-    // for the others of the wavefront the factor is 1.
+  };
+  // The reference follows the maximum only where that has left it 2^8 behind: probabilities up to 256 lose nothing in fp32
+  // sums or by a rounding to the storage type, and the accumulators are hardly ever scaled.  A row decides for itself: for the
+  // others of the wavefront the factor is 1.  Returns what the exponents are taken from.
+  const auto follow = [&](float top) {
+    top = max_of_halves(BIAS ? top : top * scale2);
     if (__any(top > m + 8.f)) {
       const float now = top > m + 8.f ? top : m;
       const float shrink = now == m ? 1.f : exp2_fast(m - now);
@@ -178,23 +146,68 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] *= shrink;
     }
-    const float base = m == -kInf ? 0.f : m;  // (a row that has seen nothing yet: every probability 0)
+    return m == -kInf ? 0.f : m;  // (a row that has seen nothing yet: every probability 0)
+  };
+  const auto largest = [&](const floatx16_t& s) {
+    float top = -kInf;
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
+    return top;
+  };
+  const auto form_scores = [&](const T* kt, const T* vt, floatx16_t& s) {
+    first_frags(kt, vt, 0);
+    s = floatx16_t{};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[b][i] = exp2_fast(BIAS ? s[b][i] - base : __builtin_fmaf(s[b][i], scale2, -base));
-        total += s[b][i];
-      }
-#pragma unroll
-      for (int c = 0; c < L::kGroups; ++c) {
-        if (c % kAhead == 0 && (b != 0 || c != 0)) read_values(b, c);
-        const typename Op::Frag p = Op::from_acc(s[b], c);
-#pragma unroll
-        for (int e = 0; e < DP / 32; ++e) Op::mma(o[e], vf[c % kAhead][e], p);
-      }
+    for (int i = 0; i < L::kSteps; ++i) {
+      Op::mma(s, ring[i % kRing], qf[i]);
+      if (i + kRing < L::kSteps) ring[i % kRing] = frag(kt, vt, i + kRing);
+      in_order();
     }
   };
+  // s: the tile's logits, with `top` their largest; kt: the next tile's keys, of which it leaves the logits in `next`.
+  const auto attend = [&](const T* kt, const T* vt, floatx16_t& s, floatx16_t& next, int next_key0, float& top, auto has_next) {
+    constexpr bool NEXT = decltype(has_next)::value;
+    first_frags(kt, vt, NEXT ? 0 : L::kSteps);
+    const float base = follow(top);
+    typename Op::Frag p[L::kGroups];
+    if (NEXT) next = floatx16_t{};
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i) {
+      if (NEXT) {
+        Op::mma(next, ring[i % kRing], qf[i]);
+        ring[i % kRing] = frag(kt, vt, i + kRing);
+      }
+#pragma unroll
+      for (int e = i * 16 / L::kSteps; e < (i + 1) * 16 / L::kSteps; ++e) {
+        s[e] = exp2_fast(BIAS ? s[e] - base : __builtin_fmaf(s[e], scale2, -base));
+        total += s[e];
+        constexpr int kGroup = 16 / L::kGroups;
+        if (e % kGroup == kGroup - 1) p[e / kGroup] = Op::from_acc(s, e / kGroup);
+      }
+      if (NEXT) {
+        if (i % 2 == 1) stay(total);
+        in_order();
+      }
+    }
+    if (NEXT) {
+#pragma unroll
+      for (int c = 0; c < L::kGroups; ++c) stay(p[c]);
+      logits(next, next_key0);
+      top = -kInf;
+    }
+#pragma unroll
+    for (int i = 0; i < kValueSteps; ++i) {
+      Op::mma(o[i % (DP / 32)], ring[i % kRing], p[i / (DP / 32)]);
+      if (i + kRing < kValueSteps) ring[i % kRing] = frag(kt, vt, L::kSteps + i + kRing);
+      if (NEXT) {
+#pragma unroll
+        for (int e = i * 16 / kValueSteps; e < (i + 1) * 16 / kValueSteps; ++e) top = fmaxf(top, next[e]);
+      }
+      in_order();
+    }
+  };
+  constexpr std::true_type yes;
+  constexpr std::false_type no;
 
   bool spoilt = false;
   float joined[DP / 8];  // SPLIT: this lane's columns of its row
@@ -207,7 +220,7 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
       // one tile of each: K's next one is requested when the scores are there, V's at the end
       T* const kt = lds + wave * 2 * kTileElems;
       T* const vt = kt + kTileElems;
-      const int tiles = last_tok / kKeys + 1;
+      const int tiles = last_tok / 32 + 1;
       if (wave < tiles) {
         load_k(kt, wave);
         load_v(vt, wave);
@@ -215,36 +228,53 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
       for (int t = wave; t < tiles; t += kWaves) {
         const bool more = t + kWaves < tiles;
         landed<Load::kLoads>();
-        attend(kt, vt, t * kKeys,
-               [&] {
-                 lds_done();
-                 if (more) load_k(kt, t + kWaves);
-               },
-               [&] {
-                 if (more) landed<Load::kLoads>();
-                 else landed<0>();
-                 if (clean) Load::clean(vt, 0, lane);
-               });
+        floatx16_t s;
+        form_scores(kt, vt, s);
+        lds_done();
+        if (more) {
+          load_k(kt, t + kWaves);
+          landed<Load::kLoads>();
+        } else {
+          landed<0>();
+        }
+        if (clean) Load::clean(vt, 0, lane);
+        logits(s, 32 * t);
+        float top = largest(s);
+        attend(kt, vt, s, s, 0, top, no);
         lds_done();
         if (more) load_v(vt, t + kWaves);
       }
     } else {
       const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);  // of the workgroup: the keys it sees
-      const int tiles = (end_tok + kKeys - 1) / kKeys;
-      load_k(lds, 0);
-      load_v(lds + kTileElems, 0);
-      for (int t = 0; t < tiles; ++t) {
-        T* const tile = lds + (t & 1) * 2 * kTileElems;
-        landed<0>();
-        if (clean) Load::clean(tile + kTileElems, part, lane);
+      const int tiles = (end_tok + 31) / 32;  // (a wavefront's last ones may be all masked: leaving them out would save nothing)
+      const auto k_tile = [&](int t) { return lds + t % S::kCopies * 2 * kTileElems; };
+      const auto v_tile = [&](int t) { return k_tile(t) + kTileElems; };
+      const auto load = [&](int t) {
+        load_k(k_tile(t), t);
+        load_v(v_tile(t), t);
+      };
+      // Tiles up to t are there, for all wavefronts, and those before t - 1 have been read: their place takes another.
+      const auto arrive = [&](int t) {
+        if (S::kCopies == 4 && t + 1 < tiles) landed<2 * Load::kLoads>();
+        else landed<0>();
+        if (clean) Load::clean(v_tile(t), part, lane);
         __syncthreads();
-        if (t + 1 < tiles) {
-          T* const next = lds + (~t & 1) * 2 * kTileElems;
-          load_k(next, t + 1);
-          load_v(next + kTileElems, t + 1);
-        }
-        if (t * kKeys <= last_tok) attend(tile, tile + kTileElems, t * kKeys, [] {}, [] {});
+        if (t + S::kCopies - 2 < tiles) load(t + S::kCopies - 2);
+      };
+      load(0);
+      if (S::kCopies == 4 && tiles > 1) load(1);
+      arrive(0);
+      floatx16_t s, next;
+      form_scores(k_tile(0), v_tile(0), s);
+      logits(s, 0);
+      float top = largest(s);
+      int t = 0;
+      for (; t + 1 < tiles; ++t) {
+        arrive(t + 1);
+        attend(k_tile(t + 1), v_tile(t), s, next, 32 * (t + 1), top, yes);
+        s = next;
       }
+      attend(k_tile(t), v_tile(t), s, s, 0, top, no);
     }
     total = sum_of_halves(total);
     if constexpr (SPLIT) {
@@ -253,23 +283,22 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
         tops[(kWaves + wave) * 32 + lane] = total;
       }
       __syncthreads();
-      float top = -kInf, own = m;
+      float top = -kInf;
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) top = fmaxf(top, tops[i * 32 + (lane & 31)]);
       total = 0.f;
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) {
-        const float of = tops[i * 32 + (lane & 31)];
-        // (a wavefront whose keys this row does not see has an empty part)
-        total += of == -kInf ? tops[(kWaves + i) * 32 + (lane & 31)] : tops[(kWaves + i) * 32 + (lane & 31)] * exp2_fast(of - top);
+        const float of = tops[i * 32 + (lane & 31)], sum = tops[(kWaves + i) * 32 + (lane & 31)];
+        total += of == -kInf ? sum : sum * exp2_fast(of - top);  // (one whose keys this row does not see has an empty part)
       }
-      m = top;
-      constexpr size_t kPartFloats = static_cast<size_t>(DP) * 32;
       float* const parts = reinterpret_cast<float*>(smem_raw);
-      static_assert(kWaves * kPartFloats * sizeof(float) <= S::kTiles, "the parts take the tiles' place");
-      write_part<DP>(parts + wave * (2 * kTileElems * sizeof(T) / sizeof(float)), o, own == -kInf ? 1.f : exp2_fast(own - top), lane);
+      constexpr size_t kPart = 2 * kTileElems * sizeof(T) / sizeof(float);
+      static_assert(32 * DP <= kPart, "the parts take the tiles' place");
+      write_part<DP>(parts + wave * kPart, o, m == -kInf ? 1.f : exp2_fast(m - top), lane);
+      m = top;
       __syncthreads();
-      join_parts<DP>(parts, 2 * kTileElems * sizeof(T) / sizeof(float), wave, lane, joined);
+      join_parts<DP>(parts, kPart, wave, lane, joined);
     }
     if (clean) break;
     float check = total * 0.f;
@@ -278,9 +307,9 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
       for (int c = 0; c < DP / 8; ++c) check = __builtin_fmaf(joined[c], 0.f, check);
     } else {
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
+      for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) check = __builtin_fmaf(o[b][i], 0.f, check);
+        for (int i = 0; i < 16; ++i) check = __builtin_fmaf(o[b][i], 0.f, check);
     }
     check = sum_of_halves(check);
     spoilt = there && check != 0.f;
