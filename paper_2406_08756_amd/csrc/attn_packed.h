@@ -311,6 +311,16 @@ __device__ __forceinline__ void load_to_lds(const RowBuffer& b, uint32_t offset,
                : "=&s"(kept) : "s"(at), "v"(offset), "s"(b.rsrc) : "memory");
 #endif
 }
+// ... of 4 bytes per lane, at `to` + 4 lane
+__device__ __forceinline__ void load_word_to_lds(const RowBuffer& b, uint32_t offset, const void* to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef const __attribute__((address_space(3))) void* lds_ptr_t;
+  const uint32_t at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)(to))));
+  uint32_t kept;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(kept) : "s"(at), "v"(offset), "s"(b.rsrc) : "memory");
+#endif
+}
 // Waits until at most N of this wavefront's loads are in flight; with LDS, until its LDS accesses are done too.
 template <int N>
 __device__ __forceinline__ void landed() {

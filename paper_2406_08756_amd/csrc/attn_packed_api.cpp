@@ -113,7 +113,7 @@ lynx_status lynx_attention_forward(const lynx_attention_config* cfg, const void*
 size_t lynx_attention_backward_bytes(const lynx_attention_config* cfg) {
   PackedAttn g;
   if (make_args(cfg, true, &g) != LYNX_OK) return 0;
-  return delta_bytes(g) + (g.buckets > 0 ? partials_bytes(g) : 0);
+  return 2 * delta_bytes(g) + (g.buckets > 0 ? partials_bytes(g) : 0);
 }
 
 lynx_status lynx_attention_backward(const lynx_attention_config* cfg, const void* q, const void* k, const void* v, const int32_t* offsets,
@@ -131,10 +131,11 @@ lynx_status lynx_attention_backward(const lynx_attention_config* cfg, const void
   g.q = q; g.k = k; g.v = v; g.offsets = offsets; g.out = const_cast<void*>(out); g.lse = const_cast<float*>(lse);
   g.d_out = d_out; g.dq = d_q; g.dk = d_k; g.dv = d_v;
   g.delta = static_cast<float*>(workspace);
+  g.offset = g.delta + delta_bytes(g) / sizeof(float);
   if (g.buckets > 0) {
     g.table = bias_table;
     g.d_table = d_bias_table;
-    g.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(g));
+    g.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * delta_bytes(g));
   }
   return lynx::attn_packed_bwd(cfg->dtype, g, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? LYNX_OK : LYNX_ERR_HIP;
 }

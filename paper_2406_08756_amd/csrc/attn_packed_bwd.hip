@@ -28,13 +28,13 @@ template <typename T, int DP, bool BIAS, bool SPLIT> struct Rows {
   static constexpr size_t kLds = kTiles + (SPLIT ? kWaves * sizeof(uint32_t) : 0);
 };
 template <typename T, int DP, bool SPLIT> struct Keys {
-  static constexpr int kRows = sizeof(T) == 2 && !SPLIT ? 64 : 32;
-  static constexpr int kTileElems = kRows * DP;
-  static constexpr size_t kTiles = (SPLIT ? 2 * kWaves : 4) * static_cast<size_t>(kTileElems) * sizeof(T);
-  static constexpr size_t kLds = kTiles + (SPLIT ? 2 * kWaves : 4) * kRows * sizeof(float) + (SPLIT ? kWaves * sizeof(uint32_t) : 0);
+  static constexpr int kTileElems = 32 * DP, kCopies = SPLIT ? kWaves : sizeof(T) * DP == 512 ? 3 : 4;
+  static constexpr size_t kTiles = 2 * kCopies * static_cast<size_t>(kTileElems) * sizeof(T);
+  static constexpr int kStat = 2 * kWave;  // floats of a tile's statistics: offset, delta, each as a wavefront loads them
+  static constexpr size_t kLds = kTiles + kCopies * kStat * sizeof(float) + (SPLIT ? kWaves * sizeof(uint32_t) : 0);
 };
 
-// The statistic as the exponent's offset; a row that sees nothing but minus infinity has probabilities of zero.
+// What the exponents are less by; a row that sees nothing but minus infinity has probabilities of zero.
 __device__ __forceinline__ float offset2(float lse) { return lse == -kInf ? kInf : lse * kLog2e; }
 
 // One row's dQ again, pair by pair, if it sees an infinity or NaN in K.
@@ -285,7 +285,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   };
   const bool one_tile = last_tok >= 0 && last_tok < 32;
   const auto write_delta = [&] {
-    if (there && half == 0 && (!SPLIT || wave == 0)) g.delta[static_cast<long long>(head0 + hp) * g.tokens + w.start + tok] = delta;
+    if (there && half == 0 && (!SPLIT || wave == 0)) {
+      const long long stat = static_cast<long long>(head0 + hp) * g.tokens + w.start + tok;
+      g.delta[stat] = delta;
+      g.offset[stat] = -lse2;
+    }
   };
   constexpr std::true_type yes;
   constexpr std::false_type no;
@@ -466,15 +470,20 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
   typedef Keys<T, DP, SPLIT> S;
-  constexpr int kRows = S::kRows, kTileElems = S::kTileElems, kKeysLog = rows_log(SPLIT);
+  constexpr int kTileElems = S::kTileElems, kKeysLog = rows_log(SPLIT);
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   T* const lds = reinterpret_cast<T*>(smem_raw);
   float* const stats = reinterpret_cast<float*>(smem_raw + S::kTiles);  // offsets and deltas, like the tiles
   float* const bias = reinterpret_cast<float*>(smem_raw + S::kLds);
 
-  const int kv = static_cast<int>(blockIdx.x) % g.kv_heads;
+  const int kv = static_cast<int>(blockIdx.x) % g.kv_heads, slot = static_cast<int>(blockIdx.x) / g.kv_heads;
   SeqTile w;
-  if (!find_tile</*LAST_FIRST=*/false>(g, static_cast<int>(blockIdx.x) / g.kv_heads, kKeysLog, 0, &w)) return;
+  if (SPLIT || g.sequences > kRankedSequences) {
+    if (!find_tile</*LAST_FIRST=*/false>(g, slot, kKeysLog, 0, &w)) return;
+  } else {
+    if (!find_ranked_tile(g, slot, kKeysLog, 0, &w)) return;
+    w.tile = ((w.len + (1 << kKeysLog) - 1) >> kKeysLog) - 1 - w.tile;  // (the first keys are seen by the most rows)
+  }
 
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -497,98 +506,160 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
     load_row_frags<T, DP>(buffer(v, g.v_stride), static_cast<uint32_t>(lane & 31) * static_cast<uint32_t>(g.v_stride) * static_cast<uint32_t>(sizeof(T)), g.d, lane, vf);
   }
   const int first_row = tile_key0 << g.pack, rows = w.len << g.pack;
-  const int tiles = (rows - first_row + kRows - 1) / kRows, steps = tiles * subs;
+  const int tiles = (rows - first_row + 31) / 32, steps = tiles * subs;
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
-  typedef Stage<T, DP, kRows, kTogether> Load;
+  typedef Stage<T, DP, 32, kTogether> Load;
   const int part = SPLIT ? 0 : wave;  // of a tile's load
-  const int who = SPLIT ? lane : static_cast<int>(threadIdx.x);
-  float next_lse = kInf, next_delta = 0.f;
-  const auto load = [&](T* tile, int it) {
-    const int sub = it / tiles, r0 = first_row + it % tiles * kRows;
+  // 32 rows of Q and d_out to `tile`, their statistics to `stat`: what is not there becomes zeros, which add nothing
+  const auto load = [&](T* tile, float* stat, int it) {
+    const int sub = it / tiles, r0 = first_row + it % tiles * 32;
     Load::rows(tile, q + static_cast<long long>(sub << g.pack) * g.d, g.q_stride, r0, w.len, g.d, g.pack, part, lane);
     Load::rows(tile + kTileElems, d_out + static_cast<long long>(sub << g.pack) * g.d, g.out_stride, r0, w.len, g.d, g.pack, part, lane);
-  };
-  const auto load_stats = [&](int it) {
-    if (who < kRows) {
-      const int sub = it / tiles, r = first_row + it % tiles * kRows + who;
-      next_lse = kInf;  // (rows behind the last: probabilities of zero)
-      next_delta = 0.f;
-      if (r < rows) {
-        const long long stat = static_cast<long long>(kv * group + (sub << g.pack) + (r & (heads - 1))) * g.tokens + w.start + (r >> g.pack);
-        next_lse = offset2(g.lse[stat]);
-        next_delta = g.delta[stat];
-      }
+    if (part == 0) {
+      const long long first = static_cast<long long>(kv * group + (sub << g.pack)) * g.tokens + w.start + (r0 >> g.pack);
+      const int row = r0 + lane;
+      const uint32_t off = lane < 32 && row < rows ? (static_cast<uint32_t>(row & (heads - 1)) * static_cast<uint32_t>(g.tokens) + (row >> g.pack) - (r0 >> g.pack)) * 4u : kOutside;
+      load_word_to_lds(row_buffer(g.offset + first, kOutside), off, stat);
+      load_word_to_lds(row_buffer(g.delta + first, kOutside), off, stat + kWave);
     }
   };
-  const auto store_stats = [&](float* stat) {
-    if (who < kRows) {
-      stat[who] = next_lse;
-      stat[kRows + who] = next_delta;
-    }
-  };
+  constexpr int kMostLoads = 2 * Load::kLoads + 2;  // (of the wavefront that has the statistics; the others have two less)
 
   floatx16_t dk[DP / 32], dv[DP / 32];
-  const uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
-  // 32 rows from r0 on, rows b0.. of qt, gt and of the statistics
-  const auto attend = [&](const T* qt, const T* gt, const float* lse_t, int b0, int r0) {
-    const int first_tok = r0 >> g.pack;
-    typename Op::Frag q_rows[L::kSteps], g_rows[L::kSteps];
+  uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
+  // A tile of 32 rows goes by in three passes of matrix instructions, with the arithmetic between them: d_out V^T, and the
+  // probabilities; the next tile's scores, and ds; dV += P^T d_out and dK += dS^T Q, and the next tile's exponents' offsets.
+  // The order is written out as in the kernel above.
+  constexpr int kRing = sizeof(T) == 2 && DP == 128 ? 8 : 4;
+  constexpr int kCols = 2 * L::kGroups * (DP / 32), kFrags = 2 * L::kSteps + kCols;
+  typename Op::Frag ring[kRing];
+  // the fragments of the three passes: of d_out, of the next tile's Q, of d_out and Q in turn
+  const auto frag = [&](const T* tile, const T* next_tile, int i) {
+    if (i < L::kSteps) return L::row_frag(tile + kTileElems, row_base, 0, i);
+    if (i < 2 * L::kSteps) return L::row_frag(next_tile, row_base, 0, i - L::kSteps);
+    const int j = i - 2 * L::kSteps;
+    return L::col_frag(j % 2 == 0 ? tile + kTileElems : tile, col_base, 0, j / 2 / (DP / 32), j / 2 % (DP / 32));
+  };
+  const auto first_frags = [&](const T* tile, const T* next_tile, int first) {
+    forget(row_base);
+    forget(col_base);
 #pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) q_rows[c] = L::row_frag(qt, row_base, b0, c);
-#pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) g_rows[c] = L::row_frag(gt, row_base, b0, c);
+    for (int i = 0; i < kRing; ++i) ring[i] = frag(tile, next_tile, first + i);
     in_order();
-    floatx16_t s{}, dp{};
+  };
+  const auto form_scores = [&](const T* tile, floatx16_t& s) {
+    first_frags(tile, tile, L::kSteps);
+    s = floatx16_t{};
 #pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) Op::mma(s, q_rows[c], kf[c]);
-#pragma unroll
-    for (int c = 0; c < L::kSteps; ++c) Op::mma(dp, g_rows[c], vf[c]);
-    constexpr int kAhead = sizeof(T) == 2 ? L::kGroups : 1;
-    typename Op::Frag g_cols[kAhead][DP / 32], q_cols[kAhead][DP / 32];
-    const auto read_cols = [&](int c0) {
-#pragma unroll
-      for (int c = 0; c < kAhead; ++c)
-#pragma unroll
-        for (int e = 0; e < DP / 32; ++e) {
-          g_cols[c][e] = L::col_frag(gt, col_base, b0, c0 + c, e);
-          q_cols[c][e] = L::col_frag(qt, col_base, b0, c0 + c, e);
-        }
-    };
-    read_cols(0);
-    in_order();
-    // register i: token first_tok + (i's part, the same for all lanes) + (4 half >> pack), head likewise
-    const int apart = first_tok + ((4 * half) >> g.pack) - key;
-    const int stride = BIAS ? table_stride(g) : 0;
-    const float* const my_bias = BIAS ? bias + kPad + (g.pack == 3 ? 4 * half * stride : 0) : nullptr;
-    const bool near = BIAS && first_tok - (key0 + 31) < g.far, edge = key0 + 31 > first_tok;
+    for (int i = 0; i < L::kSteps; ++i) {
+      Op::mma(s, ring[i % kRing], kf[i]);
+      if (i + kRing < L::kSteps) ring[i % kRing] = frag(tile, tile, L::kSteps + i + kRing);
+      in_order();
+    }
+  };
+  // register i of a tile from row r0 on: token r0 >> pack + (i's part, the same for all lanes) + (4 half >> pack), head likewise
+  const int lane_tok = ((4 * half) >> g.pack) - key, stride = BIAS ? table_stride(g) : 0;
+  const float* const my_bias = BIAS ? bias + kPad + (g.pack == 3 ? 4 * half * stride : 0) : nullptr;
+  // what a tile's registers need of its rows: the exponents' offsets without the bias (at 0) or delta (at kWave)
+  const auto per_row = [&](const float* stat, floatx16_t& x) {
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
-      const float4 lse4 = *reinterpret_cast<const float4*>(lse_t + b0 + 8 * a + 4 * half);
-      const float4 delta4 = *reinterpret_cast<const float4*>(lse_t + kRows + b0 + 8 * a + 4 * half);
-      const float lse[4] = {lse4.x, lse4.y, lse4.z, lse4.w}, delta[4] = {delta4.x, delta4.y, delta4.z, delta4.w};
+      const float4 v = *reinterpret_cast<const float4*>(stat + 8 * a + 4 * half);
+      x[4 * a] = v.x;
+      x[4 * a + 1] = v.y;
+      x[4 * a + 2] = v.z;
+      x[4 * a + 3] = v.w;
+    }
+  };
+  // registers first.. of the bias of the tile from row r0 on
+  const auto read_bias = [&](int r0, int first, int end, floatx16_t& x) {
+    const int apart = (r0 >> g.pack) + lane_tok;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 4 * a + j, ahead = (8 * a + j) >> g.pack;
-        float offset = -lse[j];
-        if (BIAS) offset += my_bias[(j & (heads - 1)) * stride + (near ? apart + ahead : g.far)];
-        const float p = exp2_fast(__builtin_fmaf(s[i], scale2, offset));
-        const bool hidden = edge && apart + ahead < 0;
-        s[i] = hidden ? 0.f : p;
-        dp[i] = hidden ? 0.f : p * (dp[i] - delta[j]);
+    for (int i = first; i < end; ++i) x[i] = my_bias[(i & 3 & (heads - 1)) * stride + min(apart + (acc_row(i, 0) >> g.pack), g.far)];
+  };
+  const auto offsets = [&](const float* stat, int r0, floatx16_t& offset) {
+    per_row(stat, offset);
+    if (BIAS) {
+      floatx16_t x;
+      read_bias(r0, 0, 16, x);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) offset[i] += x[i];
+    }
+  };
+  // s: the scores of the tile from row r0 on, `offset` their offsets; leaves those of the next one in `next` and `offset`.
+  const auto attend = [&](const T* tile, const float* stat, int r0, const T* next_tile, const float* next_stat, int next_r0, floatx16_t& s,
+                          floatx16_t& next, floatx16_t& offset, auto has_next) {
+    constexpr bool NEXT = decltype(has_next)::value;
+    first_frags(tile, next_tile, 0);
+    const auto turn = [&](int i) {  // the i-th of the fragments that are used has been: without a next tile its own are left out
+      const int n = NEXT || i + kRing < L::kSteps ? i + kRing : i + kRing + L::kSteps;
+      if (n < kFrags) ring[i % kRing] = frag(tile, next_tile, n);
+    };
+    floatx16_t dp{}, delta, next_bias;  // (read ahead of their use, as the fragments are)
+    per_row(stat + kWave, delta);
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i) {
+      Op::mma(dp, ring[i % kRing], vf[i]);
+      turn(i);
+#pragma unroll
+      for (int e = i * 16 / L::kSteps; e < (i + 1) * 16 / L::kSteps; ++e) {
+        float p = exp2_fast(__builtin_fmaf(s[e], scale2, offset[e]));
+        stay(p);
+        s[e] = p;
       }
+      in_order();
+    }
+    const int apart = (r0 >> g.pack) + lane_tok;
+    const bool edge = key0 + 31 > r0 >> g.pack;
+    if (edge) {  // (by a choice: what is masked may be NaN)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (apart + (acc_row(e, 0) >> g.pack) < 0) s[e] = 0.f;
+    }
+    typename Op::Frag p[L::kGroups], ds[L::kGroups];
+    if (NEXT) next = floatx16_t{};
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i) {
+      if (NEXT) {
+        Op::mma(next, ring[i % kRing], kf[i]);
+        turn(L::kSteps + i);
+      }
+#pragma unroll
+      for (int e = i * 16 / L::kSteps; e < (i + 1) * 16 / L::kSteps; ++e) {
+        float x = s[e] * (dp[e] - delta[e]);
+        if (NEXT) stay(x);
+        dp[e] = x;
+      }
+      if (NEXT && BIAS) read_bias(next_r0, i * 16 / L::kSteps, (i + 1) * 16 / L::kSteps, next_bias);
+      if (NEXT) in_order();
+    }
+    if (edge) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (apart + (acc_row(e, 0) >> g.pack) < 0) dp[e] = 0.f;
     }
 #pragma unroll
     for (int c = 0; c < L::kGroups; ++c) {
-      if (c != 0 && c % kAhead == 0) read_cols(c);
-      const typename Op::Frag p = Op::from_acc(s, c), ds = Op::from_acc(dp, c);
+      p[c] = Op::from_acc(s, c);
+      ds[c] = Op::from_acc(dp, c);
+    }
+    if (NEXT) per_row(next_stat, offset);
 #pragma unroll
-      for (int e = 0; e < DP / 32; ++e) {
-        Op::mma(dv[e], g_cols[c % kAhead][e], p);
-        Op::mma(dk[e], q_cols[c % kAhead][e], ds);
+    for (int i = 0; i < kCols; ++i) {
+      const int c = i / 2 / (DP / 32), e = i / 2 % (DP / 32);
+      if (i % 2 == 0) Op::mma(dv[e], ring[i % kRing], p[c]);
+      else Op::mma(dk[e], ring[i % kRing], ds[c]);
+      turn((NEXT ? 2 : 1) * L::kSteps + i);
+      if (NEXT && BIAS) {
+#pragma unroll
+        for (int n = i * 16 / kCols; n < (i + 1) * 16 / kCols; ++n) offset[n] += next_bias[n];
       }
+      in_order();
     }
   };
+  constexpr std::true_type yes;
+  constexpr std::false_type no;
 
   bool spoilt = false;
   float joined_k[DP / 8], joined_v[DP / 8];  // SPLIT: this lane's columns of its key
@@ -597,27 +668,22 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
     for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = floatx16_t{};
     if constexpr (SPLIT) {
       T* const mine = lds + wave * 2 * kTileElems;
-      float* const stat = stats + wave * 2 * kRows;
+      float* const stat = stats + wave * S::kStat;
       const auto range = [&](int first, int end) {
-        if (first + wave < end) {
-          load(mine, first + wave);
-          load_stats(first + wave);
-        }
+        if (first + wave < end) load(mine, stat, first + wave);
         for (int it = first + wave; it < end; it += kWaves) {
-          wave_fence();
-          store_stats(stat);
           landed<0>();
           if (clean) {
             Load::clean(mine, 0, lane);
             Load::clean(mine + kTileElems, 0, lane);
           }
-          wave_fence();
-          attend(mine, mine + kTileElems, stat, 0, first_row + it % tiles * kRows);
+          const int r0 = first_row + it % tiles * 32;
+          floatx16_t s, offset;
+          form_scores(mine, s);
+          offsets(stat, r0, offset);
+          attend(mine, stat, r0, mine, stat, r0, s, s, offset, no);
           lds_done();
-          if (it + kWaves < end) {
-            load(mine, it + kWaves);
-            load_stats(it + kWaves);
-          }
+          if (it + kWaves < end) load(mine, stat, it + kWaves);
         }
       };
       if (BIAS) {
@@ -642,31 +708,41 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
       __syncthreads();
       join_parts<DP>(parts, kPart, wave, lane, joined_k);
     } else {
-      load(lds, 0);
-      load_stats(0);
-      for (int it = 0; it < steps; ++it) {
-        T* const tile = lds + (it & 1) * 2 * kTileElems;
-        float* const stat = stats + (it & 1) * 2 * kRows;
-        store_stats(stat);
-        landed<0>();
-        if (clean) {
-          Load::clean(tile, part, lane);
-          Load::clean(tile + kTileElems, part, lane);
+      const auto tile = [&](int it) { return lds + it % S::kCopies * 2 * kTileElems; };
+      const auto stat = [&](int it) { return stats + it % S::kCopies * S::kStat; };
+      const auto first_of = [&](int it) { return first_row + it % tiles * 32; };
+      // Tiles up to `it` are there, for all wavefronts, and those before it - 1 have been read: their place takes another.
+      const auto arrive = [&](int it) {
+        if (S::kCopies == 4 && it + 1 < steps) {
+          if (part == 0) landed<kMostLoads>();
+          else landed<kMostLoads - 2>();
+        } else {
+          landed<0>();
         }
-        const int sub = it / tiles, r0 = first_row + it % tiles * kRows;
+        if (clean) {
+          Load::clean(tile(it), part, lane);
+          Load::clean(tile(it) + kTileElems, part, lane);
+        }
         if (BIAS && it % tiles == 0) {
-          __syncthreads();  // (the last tile of the heads before is done with their bias)
-          fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
+          __syncthreads();  // (the offsets of the heads before are done)
+          fill_bias<T, kThreads>(g, kv * group + (it / tiles << g.pack), bias);
         }
         __syncthreads();
-        if (it + 1 < steps) {
-          load(lds + (~it & 1) * 2 * kTileElems, it + 1);
-          load_stats(it + 1);
-        }
-#pragma unroll
-        for (int b = 0; b < kRows / 32; ++b)
-          if ((r0 + 32 * b + 31) >> g.pack >= key0) attend(tile, tile + kTileElems, stat, 32 * b, r0 + 32 * b);
+        if (it + S::kCopies - 2 < steps) load(tile(it + S::kCopies - 2), stat(it + S::kCopies - 2), it + S::kCopies - 2);
+      };
+      load(tile(0), stat(0), 0);
+      if (S::kCopies == 4 && steps > 1) load(tile(1), stat(1), 1);
+      arrive(0);
+      floatx16_t s, next, offset;
+      form_scores(tile(0), s);
+      offsets(stat(0), first_row, offset);
+      int it = 0;
+      for (; it + 1 < steps; ++it) {
+        arrive(it + 1);
+        attend(tile(it), stat(it), first_of(it), tile(it + 1), stat(it + 1), first_of(it + 1), s, next, offset, yes);
+        s = next;
       }
+      attend(tile(it), stat(it), first_of(it), tile(it), stat(it), first_of(it), s, s, offset, no);
     }
     if (clean) break;
     float check = 0.f;
@@ -701,7 +777,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
       }
   }
   uint32_t spoilt_keys = static_cast<uint32_t>(__ballot(spoilt));
-  if constexpr (SPLIT) spoilt_keys = share_rows(spoilt_keys, reinterpret_cast<uint32_t*>(stats + 2 * kWaves * kRows), wave);
+  if constexpr (SPLIT) spoilt_keys = share_rows(spoilt_keys, reinterpret_cast<uint32_t*>(stats + kWaves * S::kStat), wave);
   if (spoilt_keys != 0) __threadfence();
   for (uint32_t keys = spoilt_keys; keys != 0; keys &= keys - 1) {
     const int j = key0 + __builtin_ctz(keys);

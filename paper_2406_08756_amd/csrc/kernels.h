@@ -240,6 +240,7 @@ struct PackedAttn {
   const void* d_out;       // backward only, from here
   void *dq, *dk, *dv, *d_table;
   float* delta;            // [heads, tokens]: sum over d of d_out out
+  float* offset;           // [heads, tokens]: -lse log2 e
   float* partials;         // [row tiles, heads, buckets] of the table's gradient
   long long q_stride, k_stride, v_stride, out_stride, dq_stride, dk_stride, dv_stride;  // elements between tokens
   int sequences, tokens, heads, kv_heads, d;
