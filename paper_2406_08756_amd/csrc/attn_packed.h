@@ -298,28 +298,26 @@ template <typename T, int DP> struct Tile {
 // Byte offset that every row buffer reads as zero.
 constexpr uint32_t kOutside = 0x80000000u;
 
-// One 16-byte load per lane straight into LDS, at `to` (uniform) + 16 lane; outside the buffer it stores zeros.  Written out
-// because the compiler takes every LDS read behind such a load, as a builtin, to wait for it: here a tile is read while the
-// next one is on its way.  The load has no result register; landed() is the wait, and other wavefronts need a barrier after
-// it.  (Loads that the compiler counts are only waited for the longer.)
-__device__ __forceinline__ void load_to_lds(const RowBuffer& b, uint32_t offset, const void* to) {
+// One 16-byte load per lane straight into LDS, at the address `to` (uniform) + 16 lane; outside the buffer it stores zeros.
+// Written out because the compiler takes every LDS read behind such a load, as a builtin, to wait for it: here a tile is read
+// while the next one is on its way.  The load has no result register; landed() is the wait, and other wavefronts need a
+// barrier after it.  (Loads that the compiler counts are only waited for the longer.  Nothing else in these kernels uses M0,
+// which the load takes its place from.)
+__device__ __forceinline__ void load_to_lds(const RowBuffer& b, uint32_t offset, uint32_t to) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  typedef const __attribute__((address_space(3))) void* lds_ptr_t;
-  const uint32_t at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)(to))));
-  uint32_t kept;  // (M0, which the load takes its place from, is the compiler's)
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
-               : "=&s"(kept) : "s"(at), "v"(offset), "s"(b.rsrc) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(b.rsrc) : "memory");
 #endif
 }
 // ... of 4 bytes per lane, at `to` + 4 lane
-__device__ __forceinline__ void load_word_to_lds(const RowBuffer& b, uint32_t offset, const void* to) {
+__device__ __forceinline__ void load_word_to_lds(const RowBuffer& b, uint32_t offset, uint32_t to) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  typedef const __attribute__((address_space(3))) void* lds_ptr_t;
-  const uint32_t at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)(to))));
-  uint32_t kept;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
-               : "=&s"(kept) : "s"(at), "v"(offset), "s"(b.rsrc) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(b.rsrc) : "memory");
 #endif
+}
+// The address that the loads above take.
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  typedef const __attribute__((address_space(3))) void* lds_ptr_t;
+  return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)(p))));
 }
 // Waits until at most N of this wavefront's loads are in flight; with LDS, until its LDS accesses are done too.
 template <int N>
@@ -328,32 +326,40 @@ __device__ __forceinline__ void landed() {
 }
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// ROWS rows to a tile by THREADS threads (`wave`: which wavefront of them).
-template <typename T, int DP, int ROWS, int THREADS> struct Stage {
+// Tiles of 32 rows, one after another, by THREADS threads (`wave`: which wavefront of them).  What a tile's loads need is kept
+// and moved along: 64-bit multiplications and divisions per tile were a third of a wavefront's instructions.
+template <typename T, int DP, int THREADS> struct Stream {
   typedef Tile<T, DP> L;
-  static constexpr int kLoads = ROWS * L::kChunks / THREADS;
-  static_assert(ROWS * L::kChunks % THREADS == 0 && THREADS % kWave == 0, "a tile splits over the wavefronts");
-  // keys: rows first.. of `base` (row 0's first element), `rows` of which exist; zeros behind them and behind column d
-  __device__ static __forceinline__ void keys(T* tile, const T* base, long long stride, int first, int rows, int d, int wave, int lane) {
-    const int left = min(rows - first, ROWS);
-    const RowBuffer b = row_buffer(base + first * stride, left > 0 ? static_cast<uint32_t>((left - 1) * stride + d) * static_cast<uint32_t>(sizeof(T)) : 0u);
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const int e = wave * kWave + lane + THREADS * j, row = e / L::kChunks, col = (e % L::kChunks ^ L::swizzle(row)) * L::kChunk;
-      const uint32_t off = (static_cast<uint32_t>(row) * static_cast<uint32_t>(stride) + col) * static_cast<uint32_t>(sizeof(T));
-      load_to_lds(b, col < d ? off : kOutside, tile + (wave * kWave + THREADS * j) * L::kChunk);
-    }
-  }
-  // the same of rows that are (token, head) pairs; `first` is a whole token's
-  __device__ static __forceinline__ void rows(T* tile, const T* base, long long stride, int first, int tokens, int d, int pack, int wave, int lane) {
-    const int token = first >> pack, left = min(tokens - token, max(ROWS >> pack, 1)), heads = 1 << pack;
-    const RowBuffer b = row_buffer(base + token * stride, left > 0 ? static_cast<uint32_t>((left - 1) * stride + heads * d) * static_cast<uint32_t>(sizeof(T)) : 0u);
+  static constexpr int kLoads = 32 * L::kChunks / THREADS;
+  static_assert(32 * L::kChunks % THREADS == 0 && THREADS % kWave == 0, "a tile splits over the wavefronts");
+  const unsigned char* at;  // the next tile's first row
+  long long left;           // bytes from there to the end of the last row
+  uint32_t step;
+  uint32_t offset[kLoads];  // this lane's
+  // Rows are (token, head) pairs, 1 << pack heads of a token (keys: pack = 0); `base`: token 0 of `tokens`, `first`: the row that
+  // the first tile starts at, a whole token's.  Zeros come behind the last token and behind column d.
+  __device__ __forceinline__ Stream(const T* base, long long stride, int first, int tokens, int d, int pack, int wave, int lane) {
+    const int heads = 1 << pack;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       const int e = wave * kWave + lane + THREADS * j, row = e / L::kChunks, col = (e % L::kChunks ^ L::swizzle(row)) * L::kChunk;
       const uint32_t off = (static_cast<uint32_t>(row >> pack) * static_cast<uint32_t>(stride) + (row & (heads - 1)) * d + col) * static_cast<uint32_t>(sizeof(T));
-      load_to_lds(b, col < d ? off : kOutside, tile + (wave * kWave + THREADS * j) * L::kChunk);
+      offset[j] = col < d ? off : kOutside;
     }
+    step = static_cast<uint32_t>(32 >> pack) * static_cast<uint32_t>(stride) * static_cast<uint32_t>(sizeof(T));
+    start(base, stride, first, tokens, d, pack);
+  }
+  __device__ __forceinline__ void start(const T* base, long long stride, int first, int tokens, int d, int pack) {
+    at = reinterpret_cast<const unsigned char*>(base + (first >> pack) * stride);
+    left = ((tokens - 1 - (first >> pack)) * stride + (d << pack)) * static_cast<long long>(sizeof(T));
+  }
+  // the next tile to `tile` (uniform), and on by `tiles`
+  __device__ __forceinline__ void load(uint32_t tile, int wave, int tiles = 1) {
+    const RowBuffer b = row_buffer(at, left <= 0 ? 0u : left < static_cast<long long>(kOutside) ? static_cast<uint32_t>(left) : kOutside);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_to_lds(b, offset[j], tile + (wave * kWave + THREADS * j) * 16);
+    at += static_cast<unsigned long long>(step) * tiles;
+    left -= static_cast<long long>(step) * tiles;
   }
   // what this lane has loaded, without infinities and NaN
   __device__ static __forceinline__ void clean(T* tile, int wave, int lane) {

@@ -136,11 +136,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   if (SPLIT && BIAS) __syncthreads();
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
-  typedef Stage<T, DP, 32, kTogether> Load;
+  typedef Stream<T, DP, kTogether> Load;
   const int part = SPLIT ? 0 : wave;  // of a tile's load
+  const uint32_t lds_at = lds_address(smem_raw);
+  constexpr uint32_t kTileBytes = kTileElems * sizeof(T);
   floatx16_t acc[DP / 32];
-  const auto load_k = [&](T* tile, int t) { Load::keys(tile, k, g.k_stride, 32 * t, w.len, g.d, part, lane); };
-  const auto load_v = [&](T* tile, int t) { Load::keys(tile, v, g.v_stride, 32 * t, w.len, g.d, part, lane); };
   uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
   // A tile goes by in three passes of matrix instructions, with the arithmetic between them: d_out V^T, and the probabilities;
   // the next tile's scores, and ds; the sum over K.  The order is written out (in_order()), with fragments kRing steps ahead
@@ -301,12 +301,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
     for (int b = 0; b < DP / 32; ++b) acc[b] = floatx16_t{};
     if constexpr (SPLIT) {
       T* const kt = lds + wave * 2 * kTileElems;
-      const int tiles = last_tok / 32 + 1;
-      const auto load = [&](int t) {
-        load_k(kt, t);
-        load_v(kt + kTileElems, t);
+      const uint32_t k_at = lds_at + wave * 2 * kTileBytes;
+      Load k_tiles(k, g.k_stride, 32 * wave, w.len, g.d, 0, 0, lane), v_tiles(v, g.v_stride, 32 * wave, w.len, g.d, 0, 0, lane);
+      const auto load = [&] {
+        k_tiles.load(k_at, 0, kWaves);
+        v_tiles.load(k_at + kTileBytes, 0, kWaves);
       };
-      if (wave < tiles) load(wave);
+      const int tiles = last_tok / 32 + 1;
+      if (wave < tiles) load();
       for (int t = wave; t < tiles; t += kWaves) {
         landed<0>();
         if (clean) Load::clean(kt, 0, lane);
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
         if (one_tile && !clean) own_delta(kt + kTileElems, s);
         attend(kt, kt + kTileElems, kt, s, s, 32 * t, clean, no);
         lds_done();
-        if (t + kWaves < tiles) load(t + kWaves);
+        if (t + kWaves < tiles) load();
       }
       if (!clean) write_delta();
       __syncthreads();
@@ -330,11 +332,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
       const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);
       const int tiles = (end_tok + 31) / 32;
       constexpr int kKs = S::kFew ? 3 : 4, kVs = S::kFew ? 2 : 4;
-      const auto k_tile = [&](int t) { return lds + t % kKs * kTileElems; };
-      const auto v_tile = [&](int t) { return lds + (kKs + t % kVs) * kTileElems; };
-      const auto load = [&](int kt, int vt) {
-        if (kt < tiles) load_k(k_tile(kt), kt);
-        if (vt < tiles) load_v(v_tile(vt), vt);
+      const auto k_slot = [&](int t) { return t % kKs * kTileElems; };
+      const auto v_slot = [&](int t) { return (kKs + t % kVs) * kTileElems; };
+      const auto k_tile = [&](int t) { return lds + k_slot(t); };
+      const auto v_tile = [&](int t) { return lds + v_slot(t); };
+      Load k_tiles(k, g.k_stride, 0, w.len, g.d, 0, part, lane), v_tiles(v, g.v_stride, 0, w.len, g.d, 0, part, lane);
+      const auto load = [&](int kt, int vt) {  // (each in turn)
+        if (kt < tiles) k_tiles.load(lds_at + k_slot(kt) * sizeof(T), part);
+        if (vt < tiles) v_tiles.load(lds_at + v_slot(vt) * sizeof(T), part);
       };
       // K up to tile t and V up to the one before are there, for all wavefronts, and the tiles before t - 1 have been read:
       // their place takes others.
@@ -509,20 +514,46 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
   const int tiles = (rows - first_row + 31) / 32, steps = tiles * subs;
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
-  typedef Stage<T, DP, 32, kTogether> Load;
+  typedef Stream<T, DP, kTogether> Load;
   const int part = SPLIT ? 0 : wave;  // of a tile's load
-  // 32 rows of Q and d_out to `tile`, their statistics to `stat`: what is not there becomes zeros, which add nothing
-  const auto load = [&](T* tile, float* stat, int it) {
-    const int sub = it / tiles, r0 = first_row + it % tiles * 32;
-    Load::rows(tile, q + static_cast<long long>(sub << g.pack) * g.d, g.q_stride, r0, w.len, g.d, g.pack, part, lane);
-    Load::rows(tile + kTileElems, d_out + static_cast<long long>(sub << g.pack) * g.d, g.out_stride, r0, w.len, g.d, g.pack, part, lane);
+  const uint32_t lds_at = lds_address(smem_raw), stats_at = lds_address(stats);
+  constexpr uint32_t kTileBytes = kTileElems * sizeof(T), kStatBytes = S::kStat * sizeof(float);
+  // The rows of Q and d_out with their statistics, 32 at a time, `tiles` of each of the group's `subs` tiles of heads; a
+  // wavefront of a SPLIT workgroup takes every fourth of one of these.  What is not there becomes zeros, which add nothing.
+  struct Rows {
+    Load q, d_out;
+    const float *offset, *delta;  // of the next tile's first token
+    uint32_t at;                  // this lane's row
+    int row, sub, left;           // row: this lane's; left: tiles of this sub
+  };
+  const int every = SPLIT ? kWaves : 1;
+  const auto begin = [&](Rows& r, int sub, int first_tile) {
+    const long long head = kv * group + (sub << g.pack);
+    const int first = first_row + 32 * first_tile;
+    r.q.start(q + static_cast<long long>(sub << g.pack) * g.d, g.q_stride, first, w.len, g.d, g.pack);
+    r.d_out.start(d_out + static_cast<long long>(sub << g.pack) * g.d, g.out_stride, first, w.len, g.d, g.pack);
+    const long long stat = head * g.tokens + w.start + (first >> g.pack);
+    r.offset = g.offset + stat;
+    r.delta = g.delta + stat;
+    r.row = lane < 32 ? first + lane : rows;
+    r.sub = sub;
+    r.left = tiles - first_tile;
+  };
+  Rows stream{{q, g.q_stride, first_row, w.len, g.d, g.pack, part, lane}, {d_out, g.out_stride, first_row, w.len, g.d, g.pack, part, lane},
+              nullptr, nullptr, (static_cast<uint32_t>(lane & (heads - 1)) * static_cast<uint32_t>(g.tokens) + ((lane & 31) >> g.pack)) * 4u, 0, 0, 0};
+  const auto load = [&](Rows& r, uint32_t tile, uint32_t stat) {
+    if (!SPLIT && r.left <= 0) begin(r, r.sub + 1, 0);
+    r.q.load(tile, part, every);
+    r.d_out.load(tile + kTileBytes, part, every);
     if (part == 0) {
-      const long long first = static_cast<long long>(kv * group + (sub << g.pack)) * g.tokens + w.start + (r0 >> g.pack);
-      const int row = r0 + lane;
-      const uint32_t off = lane < 32 && row < rows ? (static_cast<uint32_t>(row & (heads - 1)) * static_cast<uint32_t>(g.tokens) + (row >> g.pack) - (r0 >> g.pack)) * 4u : kOutside;
-      load_word_to_lds(row_buffer(g.offset + first, kOutside), off, stat);
-      load_word_to_lds(row_buffer(g.delta + first, kOutside), off, stat + kWave);
+      const uint32_t off = r.row < rows ? r.at : kOutside;
+      load_word_to_lds(row_buffer(r.offset, kOutside), off, stat);
+      load_word_to_lds(row_buffer(r.delta, kOutside), off, stat + kWave * sizeof(float));
     }
+    r.offset += every * (32 >> g.pack);
+    r.delta += every * (32 >> g.pack);
+    r.row += every * 32;
+    r.left -= every;
   };
   constexpr int kMostLoads = 2 * Load::kLoads + 2;  // (of the wavefront that has the statistics; the others have two less)
 
@@ -669,32 +700,32 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
     if constexpr (SPLIT) {
       T* const mine = lds + wave * 2 * kTileElems;
       float* const stat = stats + wave * S::kStat;
-      const auto range = [&](int first, int end) {
-        if (first + wave < end) load(mine, stat, first + wave);
-        for (int it = first + wave; it < end; it += kWaves) {
+      const uint32_t tile_at = lds_at + wave * 2 * kTileBytes, stat_at = stats_at + wave * kStatBytes;
+      const auto of_heads = [&](int sub) {
+        begin(stream, sub, wave);
+        if (wave < tiles) load(stream, tile_at, stat_at);
+        for (int t = wave; t < tiles; t += kWaves) {
           landed<0>();
           if (clean) {
             Load::clean(mine, 0, lane);
             Load::clean(mine + kTileElems, 0, lane);
           }
-          const int r0 = first_row + it % tiles * 32;
+          const int r0 = first_row + 32 * t;
           floatx16_t s, offset;
           form_scores(mine, s);
           offsets(stat, r0, offset);
           attend(mine, stat, r0, mine, stat, r0, s, s, offset, no);
           lds_done();
-          if (it + kWaves < end) load(mine, stat, it + kWaves);
+          if (t + kWaves < tiles) load(stream, tile_at, stat_at);
         }
       };
-      if (BIAS) {
-        for (int sub = 0; sub < subs; ++sub) {
+      for (int sub = 0; sub < subs; ++sub) {
+        if (BIAS) {
           __syncthreads();  // (the heads before are done with their bias)
           fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
           __syncthreads();
-          range(sub * tiles, (sub + 1) * tiles);
         }
-      } else {
-        range(0, steps);
+        of_heads(sub);
       }
       float* const parts = reinterpret_cast<float*>(smem_raw);
       constexpr size_t kPart = 2 * kTileElems * sizeof(T) / sizeof(float);
@@ -708,9 +739,11 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
       __syncthreads();
       join_parts<DP>(parts, kPart, wave, lane, joined_k);
     } else {
-      const auto tile = [&](int it) { return lds + it % S::kCopies * 2 * kTileElems; };
-      const auto stat = [&](int it) { return stats + it % S::kCopies * S::kStat; };
-      const auto first_of = [&](int it) { return first_row + it % tiles * 32; };
+      const auto slot = [&](int it) { return it % S::kCopies; };
+      const auto tile = [&](int it) { return lds + slot(it) * 2 * kTileElems; };
+      const auto stat = [&](int it) { return stats + slot(it) * S::kStat; };
+      const auto load_next = [&](int it) { load(stream, lds_at + slot(it) * 2 * kTileBytes, stats_at + slot(it) * kStatBytes); };
+      int ahead = 0, sub = 0;  // tile `it + 1`: its number among those of its heads, and which heads
       // Tiles up to `it` are there, for all wavefronts, and those before it - 1 have been read: their place takes another.
       const auto arrive = [&](int it) {
         if (S::kCopies == 4 && it + 1 < steps) {
@@ -723,26 +756,33 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
           Load::clean(tile(it), part, lane);
           Load::clean(tile(it) + kTileElems, part, lane);
         }
-        if (BIAS && it % tiles == 0) {
+        if (BIAS && ahead == 0) {
           __syncthreads();  // (the offsets of the heads before are done)
-          fill_bias<T, kThreads>(g, kv * group + (it / tiles << g.pack), bias);
+          fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
         }
         __syncthreads();
-        if (it + S::kCopies - 2 < steps) load(tile(it + S::kCopies - 2), stat(it + S::kCopies - 2), it + S::kCopies - 2);
+        if (it + S::kCopies - 2 < steps) load_next(it + S::kCopies - 2);
       };
-      load(tile(0), stat(0), 0);
-      if (S::kCopies == 4 && steps > 1) load(tile(1), stat(1), 1);
+      begin(stream, 0, 0);
+      load_next(0);
+      if (S::kCopies == 4 && steps > 1) load_next(1);
       arrive(0);
       floatx16_t s, next, offset;
       form_scores(tile(0), s);
       offsets(stat(0), first_row, offset);
-      int it = 0;
+      int it = 0, r0 = first_row;
       for (; it + 1 < steps; ++it) {
+        if (++ahead == tiles) {
+          ahead = 0;
+          ++sub;
+        }
+        const int next_r0 = first_row + 32 * ahead;
         arrive(it + 1);
-        attend(tile(it), stat(it), first_of(it), tile(it + 1), stat(it + 1), first_of(it + 1), s, next, offset, yes);
+        attend(tile(it), stat(it), r0, tile(it + 1), stat(it + 1), next_r0, s, next, offset, yes);
         s = next;
+        r0 = next_r0;
       }
-      attend(tile(it), stat(it), first_of(it), tile(it), stat(it), first_of(it), s, s, offset, no);
+      attend(tile(it), stat(it), r0, tile(it), stat(it), r0, s, s, offset, no);
     }
     if (clean) break;
     float check = 0.f;

@@ -88,12 +88,12 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
   if (SPLIT && BIAS) __syncthreads();
 
   constexpr int kTogether = SPLIT ? kWave : kThreads;
-  typedef Stage<T, DP, 32, kTogether> Load;
+  typedef Stream<T, DP, kTogether> Load;
   const int part = SPLIT ? 0 : wave;  // of a tile's load
+  const uint32_t lds_at = lds_address(smem_raw);
+  constexpr uint32_t kTileBytes = kTileElems * sizeof(T);
   floatx16_t o[DP / 32];
   float m, total;
-  const auto load_k = [&](T* tile, int t) { Load::keys(tile, k, g.k_stride, 32 * t, w.len, g.d, part, lane); };
-  const auto load_v = [&](T* tile, int t) { Load::keys(tile, v, g.v_stride, 32 * t, w.len, g.d, part, lane); };
   uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
   // A tile goes by in two passes of matrix instructions, with the arithmetic between them: the scores of tile t + 1, and the
   // probabilities of tile t; the sum of tile t over V, and the maxima of tile t + 1.  The order is written out (in_order()), with
@@ -220,10 +220,12 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
       // one tile of each: K's next one is requested when the scores are there, V's at the end
       T* const kt = lds + wave * 2 * kTileElems;
       T* const vt = kt + kTileElems;
+      const uint32_t k_at = lds_at + wave * 2 * kTileBytes, v_at = k_at + kTileBytes;
+      Load k_tiles(k, g.k_stride, 32 * wave, w.len, g.d, 0, 0, lane), v_tiles(v, g.v_stride, 32 * wave, w.len, g.d, 0, 0, lane);
       const int tiles = last_tok / 32 + 1;
       if (wave < tiles) {
-        load_k(kt, wave);
-        load_v(vt, wave);
+        k_tiles.load(k_at, 0, kWaves);
+        v_tiles.load(v_at, 0, kWaves);
       }
       for (int t = wave; t < tiles; t += kWaves) {
         const bool more = t + kWaves < tiles;
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
         form_scores(kt, vt, s);
         lds_done();
         if (more) {
-          load_k(kt, t + kWaves);
+          k_tiles.load(k_at, 0, kWaves);
           landed<Load::kLoads>();
         } else {
           landed<0>();
@@ -242,22 +244,22 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
         float top = largest(s);
         attend(kt, vt, s, s, 0, top, no);
         lds_done();
-        if (more) load_v(vt, t + kWaves);
+        if (more) v_tiles.load(v_at, 0, kWaves);
       }
     } else {
       const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);  // of the workgroup: the keys it sees
       const int tiles = (end_tok + 31) / 32;  // (a wavefront's last ones may be all masked: leaving them out would save nothing)
-      const auto k_tile = [&](int t) { return lds + t % S::kCopies * 2 * kTileElems; };
-      const auto v_tile = [&](int t) { return k_tile(t) + kTileElems; };
+      Load k_tiles(k, g.k_stride, 0, w.len, g.d, 0, part, lane), v_tiles(v, g.v_stride, 0, w.len, g.d, 0, part, lane);
+      const auto slot = [&](int t) { return t % S::kCopies * 2 * kTileElems; };
       const auto load = [&](int t) {
-        load_k(k_tile(t), t);
-        load_v(v_tile(t), t);
+        k_tiles.load(lds_at + slot(t) * sizeof(T), part);
+        v_tiles.load(lds_at + slot(t) * sizeof(T) + kTileBytes, part);
       };
       // Tiles up to t are there, for all wavefronts, and those before t - 1 have been read: their place takes another.
       const auto arrive = [&](int t) {
         if (S::kCopies == 4 && t + 1 < tiles) landed<2 * Load::kLoads>();
         else landed<0>();
-        if (clean) Load::clean(v_tile(t), part, lane);
+        if (clean) Load::clean(lds + slot(t) + kTileElems, part, lane);
         __syncthreads();
         if (t + S::kCopies - 2 < tiles) load(t + S::kCopies - 2);
       };
@@ -265,16 +267,16 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
       if (S::kCopies == 4 && tiles > 1) load(1);
       arrive(0);
       floatx16_t s, next;
-      form_scores(k_tile(0), v_tile(0), s);
+      form_scores(lds, lds, s);
       logits(s, 0);
       float top = largest(s);
       int t = 0;
       for (; t + 1 < tiles; ++t) {
         arrive(t + 1);
-        attend(k_tile(t + 1), v_tile(t), s, next, 32 * (t + 1), top, yes);
+        attend(lds + slot(t + 1), lds + slot(t) + kTileElems, s, next, 32 * (t + 1), top, yes);
         s = next;
       }
-      attend(k_tile(t), v_tile(t), s, s, 0, top, no);
+      attend(lds + slot(t), lds + slot(t) + kTileElems, s, s, 0, top, no);
     }
     total = sum_of_halves(total);
     if constexpr (SPLIT) {
