@@ -12,9 +12,10 @@ namespace lynx {
 namespace {
 
 // The gradient of the position bias.  ds by distance, for each head of the tile and each wavefront apart: `far` distances and
-// what a 32 x 32 block that holds one of them reaches beyond.  A near block is laid down in LDS and a lane adds up one of its
-// diagonals, so that each sum has one owner and one order; blocks whose keys are all far are summed in a register.
-constexpr int kBlockStride = 33, kBlockPad = 32, kBlockFloats = 32 * kBlockStride + 2 * kBlockPad;
+// what a 32 x 32 block that holds one of them reaches beyond.  A near block is laid down in LDS by diagonals, 16 rows at a time
+// (47 diagonals; which places of a diagonal exist depends on the row alone, the others stay zero), and a lane adds up one of
+// them, so that each sum has one owner and one order.  Blocks whose keys are all far are summed in a register.
+constexpr int kDiagonalStride = 20, kBlockFloats = 47 * kDiagonalStride + 20;
 __host__ __device__ __forceinline__ int distances(const PackedAttn& g) { return g.far + 64; }
 __host__ __device__ __forceinline__ int by_distance_floats(const PackedAttn& g) { return (distances(g) << g.pack) + kBlockFloats; }  // of a wavefront
 
@@ -192,22 +193,46 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
       for (int e = 0; e < 16; ++e) far_sum += ds[e];
       return;
     }
-    float* const block = my_sums + (distances(g) << g.pack) + kBlockPad;
-    wave_fence();
+    float* const block = my_sums + (distances(g) << g.pack);
+    const int row16 = lane & 15;
+    float* const mine = block + ((row16 >> g.pack) + 4 - 4 * half) * kDiagonalStride + row16;  // (of the last key of this half)
+    const float4* const diagonal = reinterpret_cast<const float4*>(block + min(lane, 46) * kDiagonalStride);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) block[(lane & 31) * kBlockStride + acc_row(e, half)] = ds[e];
-    wave_fence();
-    // lane: the diagonal token - key = lane - 31, of each head in turn
-    const int diagonal = lane - 31, distance = first_tok - key0 + diagonal, tokens = 32 >> g.pack;
-    for (int h = 0; h < heads; ++h) {
-      float sum = 0.f;
-#pragma unroll 8
-      for (int r = 0; r < tokens; ++r) {
-        const float x = block[((r << g.pack) + h) * kBlockStride + r - diagonal];
-        sum += r - diagonal >= 0 && r - diagonal < 32 ? x : 0.f;
+    for (int r = 0; r < 2; ++r) {
+      in_order();
+      wave_fence();
+      if (((lane >> 4) & 1) == r) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mine[(27 - acc_row(e, 0)) * kDiagonalStride] = ds[e];
       }
-      if (distance >= 0 && diagonal < tokens) my_sums[h * distances(g) + distance] += sum;
+      wave_fence();
+      float sum[8];  // of the rows whose number is 0 .. 7 modulo 8
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float4 x = diagonal[j], y = diagonal[j + 2];
+        sum[4 * j] = x.x + y.x;
+        sum[4 * j + 1] = x.y + y.y;
+        sum[4 * j + 2] = x.z + y.z;
+        sum[4 * j + 3] = x.w + y.w;
+      }
+      // (a head's rows are every 2^pack-th)
+      if (g.pack < 3) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) sum[h] += sum[h + 4];
+      }
+      if (g.pack < 2) {
+        sum[0] += sum[2];
+        sum[1] += sum[3];
+      }
+      if (g.pack < 1) sum[0] += sum[1];
+      const int distance = first_tok + ((16 * r) >> g.pack) - key0 + lane - 31;
+      if (distance >= 0 && lane < 31 + (16 >> g.pack)) {
+#pragma unroll
+        for (int h = 0; h < 8; ++h)
+          if (h < heads) my_sums[h * distances(g) + distance] += sum[h];
+      }
     }
+    in_order();
   };
   // s: the exponents of the tile at kt (scores without a bias); next_kt: the next tile, of which it leaves them in `next`.
   const auto attend = [&](const T* kt, const T* vt, const T* next_kt, floatx16_t& s, floatx16_t& next, int key0, bool clean, auto has_next) {

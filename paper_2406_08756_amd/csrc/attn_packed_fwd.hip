@@ -359,22 +359,29 @@ hipError_t launch_fwd(const PackedAttn& g, hipStream_t st) {
 
 }  // namespace
 
-// Fewer workgroups of 128 rows or keys than this, and 32 each go faster.
-constexpr size_t kSplitBelow = 512;
+// Workgroups of 128 rows that the card takes at a time; with fewer, 32 rows each go faster (2048 tokens of 5 heads, 85: 26 us
+// against 62; 139 tiles of 5 heads, 695: 96 us, with 32 rows each 103).
+constexpr size_t kRowGroups = 512;
+// Of 128 keys it takes as many for heads of up to 64, half for wider ones.  They differ more in size, and it takes two rounds
+// of them to even that out (heads of 64, 576 of them: 361 us, with 32 keys each 194; 1088: 113 and 126; heads of 128, 695:
+// 170 and 215).  And sequences that are shorter than a tile leave most of one empty (256 of 32 tokens on average: 43 us and 31).
+constexpr size_t key_groups(int d) { return d <= 64 ? 512 : 256; }
+constexpr int kShort = 96;
 // As many heads of a group as are a power of two, up to 8; fewer where their biases by distance would take more than 10 KB of
 // LDS, so that with four times that for the gradient's sums and the tiles of fp32 a workgroup has what it needs.
 void attn_packed_choose(int dtype, PackedAttn* g) {
   const int group = g->heads / g->kv_heads;
   g->pack = 0;
   while (g->pack < 3 && (group >> g->pack) % 2 == 0 && (g->buckets == 0 || table_stride(*g) << (g->pack + 1) <= 2560)) ++g->pack;
-  g->split_fwd = attn_packed_row_slots(*g, false) * (g->heads >> g->pack) < kSplitBelow;
+  g->split_fwd = attn_packed_row_slots(*g, false) * (g->heads >> g->pack) < kRowGroups;
   g->split_rows = g->split_fwd && attn_packed_split_rows_fit(dtype, *g);
   g->split_keys = 0;
-  g->split_keys = attn_packed_key_slots(*g) * g->kv_heads < kSplitBelow;
+  g->split_keys = attn_packed_key_slots(*g) * g->kv_heads < 2 * key_groups(g->d) || g->tokens / g->sequences < kShort;
 }
 bool attn_packed_fits(const PackedAttn& g) {
-  const long long slots = static_cast<long long>(attn_packed_row_slots(g, g.split_fwd));
-  return fits_grid(slots * (g.heads >> g.pack), kThreads) && slots < (1ll << 31);
+  const long long subs = g.heads >> g.pack, fwd = static_cast<long long>(attn_packed_row_slots(g, g.split_fwd)) * subs;
+  const long long rows = static_cast<long long>(attn_packed_row_slots(g, g.split_rows)) * subs, keys = static_cast<long long>(attn_packed_key_slots(g)) * g.kv_heads;
+  return fits_grid(fwd, kThreads) && fits_grid(rows, kThreads) && fits_grid(keys, kThreads);
 }
 size_t attn_packed_row_slots(const PackedAttn& g, bool split) {
   return ((static_cast<size_t>(g.tokens) << g.pack) >> rows_log(split)) + static_cast<size_t>(g.sequences);
