@@ -69,6 +69,7 @@ __device__ __forceinline__ int2 sequence_span(const PackedAttn& g, int s) {
 // the most keys, start first (of key tiles, the first ones are seen by the most rows).
 // Every wavefront looks for itself; each lane sums the tiles of its share of the sequences, a prefix sum finds the share,
 // and the search goes on within it.  False if there are not that many tiles.
+constexpr int kMostTiles = 1 << 29;
 template <bool LAST_FIRST>
 __device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int tile_log, int pack, SeqTile* out) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -79,13 +80,14 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int til
     int sum = 0;
     for (int i = 0; i < per; ++i) {
       const int s = lane * per + i;
-      if (s < count) sum += ((sequence_span(g, first + s).y << pack) + (1 << tile_log) - 1) >> tile_log;
+      // (the limit: offsets that fall name rows many times, and their sum must not pass 32 bits)
+      if (s < count) sum = min(sum + (((sequence_span(g, first + s).y << pack) + (1 << tile_log) - 1) >> tile_log), kMostTiles);
     }
     int upto = sum;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
       const int v = __shfl_up(upto, o, kWave);
-      if (lane >= o) upto += v;
+      if (lane >= o) upto = min(upto + v, kMostTiles);
     }
     if (top) {
       const int total = __builtin_amdgcn_readlane(upto, kWave - 1);
