@@ -92,6 +92,15 @@ typedef struct {
  * full-recompute layer drops by about three seq x seq tensors.  Off by default. */
 #define LYNX_FLAG_FUSED_ATTENTION 1u
 
+/* Attention over packed sequences: the layer's micro_batch * seq tokens are sequences of any lengths behind one
+ * another (lynx_layer_set_sequences), causal within each, optionally with a learned position bias
+ * (lynx_layer_set_position_bias).  Operators 3 to 6 are one (lynx_attention_forward): S, P and Pd never exist, naming
+ * operators 3-5 in a segment is a no-op and their retain bits are ignored, operator 6 reads QKV alone, backward
+ * reads QKV and C, and no seq x seq tensor of any kind is formed.  The attention probabilities are not dropped out; the
+ * hidden sites (1 and 2) are as ever.  Rows of no sequence have a context and a QKV gradient of zero and go through the
+ * other operators like any token.  head_dim <= 128; not together with LYNX_FLAG_FUSED_ATTENTION. */
+#define LYNX_FLAG_PACKED_ATTENTION 2u
+
 /* Device pointers to the parameters, borrowed until the next set_params or
  * destroy.  Shapes: wqkv [3*a*d, h], bqkv [3*a*d], wo [h, a*d], bo [h],
  * w1 [f, h], b1 [f], w2 [h, f], b2 [h], LayerNorm g1, be1, g2, be2 [h]. */
@@ -175,6 +184,18 @@ lynx_status lynx_layer_create_static(const lynx_layer_config* cfg, lynx_layer_t*
 
 lynx_status lynx_layer_set_params(lynx_layer_t layer, const lynx_params* params);
 
+/* Layers with LYNX_FLAG_PACKED_ATTENTION only (else STATE; also STATE between forward and backward).
+ * Sequence i of the next passes is tokens offsets[i] .. offsets[i+1] - 1; offsets (device, sequences + 1 entries) is
+ * borrowed and read by the kernels of forward, regeneration and backward, so its values must not change in between.
+ * A forward pass without sequences fails with STATE.  Errors: INVALID_ARG, STATE, SHAPE (sequences not in
+ * 1 .. micro_batch + tokens / 16). */
+lynx_status lynx_layer_set_sequences(lynx_layer_t layer, const int32_t* offsets_device, int32_t sequences);
+/* The position bias of the next passes: bucket_starts (host, copied) as in lynx_attention_config, table_device and
+ * d_table_device [num_buckets, local_heads] in the storage type, borrowed; backward overwrites d_table_device.
+ * num_buckets 0: none.  Errors: INVALID_ARG, STATE, SHAPE. */
+lynx_status lynx_layer_set_position_bias(lynx_layer_t layer, int32_t num_buckets, const int32_t* bucket_starts,
+                                         const void* table_device, void* d_table_device);
+
 /* Forward pass (operators 1..13) under a retain policy: after an operator's
  * last forward consumer has run, its output is released unless its retain bit
  * is set.  x_device [T, h] is borrowed and must stay valid and unchanged
@@ -236,7 +257,7 @@ lynx_status lynx_layer_activation(lynx_layer_t layer, int act_id, const void** d
  *   1 dY1 [T, h]
  * in the storage dtype; device_dst holds that many elements (dS: the whole
  * dense [b, a, s, s] block is copied).  NULL clears the tap.
- * Other act_id (gradients no kernel materialises) -> INVALID_ARG. */
+ * Other act_id (gradients no kernel materialises; also 3 of a layer of packed sequences) -> INVALID_ARG. */
 lynx_status lynx_layer_set_gradient_tap(lynx_layer_t layer, int act_id, void* device_dst);
 
 /* Write the keep-mask of one dropout site as bytes (1 = keep) for parity

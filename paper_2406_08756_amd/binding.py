@@ -32,6 +32,7 @@ LYNX_NUM_ACTIVATIONS = 14
 LYNX_PROFILE_SLOTS = 40
 LYNX_STATIC_WORKSPACE_BYTES = 64 << 20
 LYNX_FLAG_FUSED_ATTENTION = 1
+LYNX_FLAG_PACKED_ATTENTION = 2
 LYNX_ATTENTION_MAX_HEAD_DIM, LYNX_ATTENTION_MAX_STRIDE = 128, 1 << 21
 LYNX_MAX_BUCKETS, LYNX_MAX_DISTANCE = 64, 2048
 PARAM_FIELDS = ("wqkv", "bqkv", "wo", "bo", "w1", "b1", "w2", "b2", "g1", "be1", "g2", "be2")
@@ -96,6 +97,8 @@ _proto = {
     "lynx_layer_create_static": (C.c_int, [_cfg_p, C.POINTER(C.c_void_p)]),
     "lynx_layer_destroy": (C.c_int, [C.c_void_p]),
     "lynx_layer_set_params": (C.c_int, [C.c_void_p, C.POINTER(lynx_params)]),
+    "lynx_layer_set_sequences": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32]),
+    "lynx_layer_set_position_bias": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.c_void_p, C.c_void_p]),
     "lynx_layer_forward": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint64,
                                      C.c_void_p]),
     "lynx_recompute": (C.c_int, [C.c_void_p, C.c_uint32, C.c_void_p]),
@@ -208,6 +211,16 @@ def _ptr_struct(cls, tensors: Dict[str, object]):
 def lynx_layer_set_params(layer: int, params: Dict[str, object]) -> None:
     st = _ptr_struct(lynx_params, params)
     _check(_lib.lynx_layer_set_params(layer, C.byref(st)), "lynx_layer_set_params")
+
+
+def lynx_layer_set_sequences(layer: int, offsets, sequences: int) -> None:
+    _check(_lib.lynx_layer_set_sequences(layer, _addr(offsets), sequences), "lynx_layer_set_sequences")
+
+
+def lynx_layer_set_position_bias(layer: int, num_buckets: int, bucket_starts=None, table=None, d_table=None) -> None:
+    """bucket_starts: a host array as lynx_position_buckets returns it."""
+    _check(_lib.lynx_layer_set_position_bias(layer, num_buckets, bucket_starts, _addr(table), _addr(d_table)),
+           "lynx_layer_set_position_bias")
 
 
 def lynx_layer_forward(layer: int, x, out, retain_mask: int, step: int = 0, stream=None) -> None:

@@ -71,6 +71,13 @@ struct Whole {
 
 }  // namespace
 
+namespace lynx {
+lynx_status attention_check(const lynx_attention_config* cfg) {
+  PackedAttn g;
+  return make_args(cfg, true, &g);
+}
+}  // namespace lynx
+
 extern "C" {
 
 lynx_status lynx_position_buckets(int num_buckets, int max_distance, int32_t* starts_out) {

@@ -341,6 +341,15 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
   }
 }
 
+// Rows outside [offsets[0], offsets[sequences]); where there are none the workgroups only look.
+__global__ void attn_packed_clear_kernel(unsigned char* x, int row_bytes, int tokens, const int32_t* offsets, int sequences) {
+  const int first = min(max(offsets[0], 0), tokens), end = min(max(offsets[sequences], first), tokens), outside = tokens - (end - first);
+  for (int r = blockIdx.x; r < outside; r += gridDim.x) {
+    unsigned char* const row = x + static_cast<long long>(r < first ? r : r - first + end) * row_bytes;
+    for (int c = threadIdx.x * 16; c < row_bytes; c += kThreads * 16) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
+  }
+}
+
 template <typename T, int DP, bool BIAS>
 hipError_t launch_fwd(const PackedAttn& g, hipStream_t st) {
   const size_t table = BIAS ? static_cast<size_t>(table_floats(g)) * sizeof(float) : 0;
@@ -388,6 +397,11 @@ size_t attn_packed_row_slots(const PackedAttn& g, bool split) {
 }
 size_t attn_packed_key_slots(const PackedAttn& g) {
   return (static_cast<size_t>(g.tokens) >> rows_log(g.split_keys)) + static_cast<size_t>(g.sequences);
+}
+hipError_t attn_packed_clear(int dtype, void* x, int cols, int tokens, const int32_t* offsets, int sequences, hipStream_t st) {
+  hipLaunchKernelGGL(attn_packed_clear_kernel, dim3(tokens < 256 ? tokens : 256), dim3(kThreads), 0, st, static_cast<unsigned char*>(x),
+                     cols * (dtype == 1 ? 2 : 4), tokens, offsets, sequences);
+  return hipGetLastError();
 }
 hipError_t attn_packed_fwd(int dtype, const PackedAttn& g, hipStream_t st) {
   return dtype == 1 ? launch_fwd<bf16_t>(g, st) : launch_fwd<float>(g, st);

@@ -252,6 +252,8 @@ struct PackedAttn {
 };
 hipError_t attn_packed_fwd(int dtype, const PackedAttn& g, hipStream_t st);
 hipError_t attn_packed_bwd(int dtype, const PackedAttn& g, hipStream_t st);
+// Zeros to the rows of x [tokens, cols] that are of no sequence.
+hipError_t attn_packed_clear(int dtype, void* x, int cols, int tokens, const int32_t* offsets, int sequences, hipStream_t st);
 // Sets `pack` and the splits from the shape.
 void attn_packed_choose(int dtype, PackedAttn* g);
 bool attn_packed_split_rows_fit(int dtype, const PackedAttn& g);

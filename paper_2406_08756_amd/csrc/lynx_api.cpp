@@ -18,6 +18,10 @@
 #include "kernels.h"
 #include "static_workspace.h"
 
+namespace lynx {
+lynx_status attention_check(const lynx_attention_config* cfg);  // attn_packed_api.cpp: whether a backward pass takes it
+}
+
 namespace {
 
 using lynx::Arena;
@@ -41,6 +45,7 @@ struct Dims {
   int dtype, e;
   int b, s, a, d, h, p, f, T;
   size_t ss;  // b * a * s * s
+  bool packed;  // LYNX_FLAG_PACKED_ATTENTION: no tensor of that size exists
 };
 
 bool make_dims(const lynx_layer_config* c, Dims* o) {
@@ -54,7 +59,10 @@ bool make_dims(const lynx_layer_config* c, Dims* o) {
   if (!(c->dropout_p >= 0.0f && c->dropout_p < 1.0f)) return false;
   if (!(c->ln_eps >= 0.0f)) return false;
   if (c->tp_size <= 0 || c->tp_rank < 0 || c->tp_rank >= c->tp_size) return false;
-  if (c->layer_id >= (1u << 30) || c->causal != 1 || (c->flags & ~LYNX_FLAG_FUSED_ATTENTION)) return false;
+  if (c->layer_id >= (1u << 30) || c->causal != 1) return false;
+  if (c->flags & ~(LYNX_FLAG_FUSED_ATTENTION | LYNX_FLAG_PACKED_ATTENTION)) return false;
+  const bool packed = (c->flags & LYNX_FLAG_PACKED_ATTENTION) != 0;
+  if (packed && (c->flags & LYNX_FLAG_FUSED_ATTENTION || c->head_dim > LYNX_ATTENTION_MAX_HEAD_DIM)) return false;
   const long long T = static_cast<long long>(c->micro_batch) * c->seq;
   if (T > (1ll << 24)) return false;
   o->dtype = c->dtype;
@@ -63,7 +71,8 @@ bool make_dims(const lynx_layer_config* c, Dims* o) {
   o->h = c->hidden; o->p = c->local_heads * c->head_dim; o->f = c->local_ffn;
   o->T = static_cast<int>(T);
   o->ss = static_cast<size_t>(o->b) * o->a * o->s * o->s;
-  return true;
+  o->packed = packed;
+  return !packed || 3ll * o->p <= LYNX_ATTENTION_MAX_STRIDE;
 }
 
 size_t act_bytes(const Dims& D, int i) {
@@ -73,7 +82,7 @@ size_t act_bytes(const Dims& D, int i) {
     case 0: case 7: case 8: case 12: case 13: return th;
     case 1: case 9: return th + stats;
     case 2: return static_cast<size_t>(D.T) * 3 * D.p * D.e;
-    case 3: case 4: case 5: return D.ss * D.e;
+    case 3: case 4: case 5: return D.packed ? 0 : D.ss * D.e;
     // C carries the attention row statistics (maximum, 1 / sum: two fp32 per row and head)
     // that the kernels which never store S, P, Pd leave for their backward
     case 6: return static_cast<size_t>(D.T) * D.p * D.e + static_cast<size_t>(D.b) * D.a * D.s * 2 * sizeof(float);
@@ -89,8 +98,8 @@ struct Book {
   size_t off[kNumAct] = {};
   uint32_t retain = 0;
   int state = 0;  // 0 idle, 1 forward done / backward pending
-  // the policy keeps none of S, P, Pd and the shape is one the fused attention kernels take:
-  // operators 3-5 never run, operator 6 reads QKV alone
+  // the policy keeps none of S, P, Pd and the shape is one the fused attention kernels take, or the sequences are
+  // packed: operators 3-5 never run, operator 6 reads QKV alone
   bool fused_attn = false;
   // Index into kGoesWithout: what the run goes without because the workspace has no room for it.  It can change
   // within a run (two_pass) and differ from one policy to the next, so no value may depend on it: every level sums
@@ -145,6 +154,15 @@ struct lynx_layer_s {
   bool ev_recorded[LYNX_PROFILE_SLOTS] = {};
   // parity aid: where backward copies the gradient with respect to activation A_i (null: nowhere)
   void* grad_tap[LYNX_NUM_ACTIVATIONS] = {};
+  // packed attention: the sequences and the position bias (borrowed; `bias.buckets` 0: none)
+  const int32_t* offsets = nullptr;
+  int sequences = 0;
+  struct {
+    int buckets = 0;
+    int32_t starts[LYNX_MAX_BUCKETS];
+    const void* table = nullptr;
+    void* d_table = nullptr;
+  } bias;
   int static_device = -1;  // >= 0: the workspace is that device's built-in block
   // per retain mask (bits 1..12) the Book::thrift that thrift_for has found, -1: not rehearsed yet.  A byte for each of
   // the 4096 masks: a caller may change policy from one micro-batch to the next.
@@ -186,7 +204,7 @@ struct Ctx {  // one pass (rehearsal or real) of a call
 enum BackwardSlot {
   kB13Dropout = 14, kB12Grads, kB11Gelu, kB10Grads, kB98LayerNormDropout, kB7Grads, kB6DPd,
   kB6DV, kB54Softmax, kB3DQ, kB3DK, kB2Grads, kB2BiasGrad, kB1LayerNorm, kB6RowDot, kB654DScores,
-  kOp36Fused, kB654DScoresFused, kB6DVFused, kColumnSums, kNumSlots
+  kOp36Fused, kB654DScoresFused, kB6DVFused, kColumnSums, kB6543Packed, kNumSlots
 };
 static_assert(kNumSlots <= LYNX_PROFILE_SLOTS, "profile slots");
 static_assert(LYNX_STATIC_WORKSPACE_BYTES == lynx::kStaticWorkspaceBytes, "header and library agree on the block size");
@@ -197,7 +215,7 @@ const char* const kSlotNames[kNumSlots] = {
     "b12_fc2_dgrad_wgrad", "b11_gelu_bwd", "b10_fc1_dgrad_wgrad",
     "b98_layernorm2_dropout_bwd", "b7_proj_dgrad_wgrad", "b6_dpd", "b6_dv", "b54_softmax_dropout_bwd", "b3_dq",
     "b3_dk", "b2_qkv_dgrad_wgrad", "b2_bias_grad", "b1_layernorm1_bwd", "b6_rowdot", "b654_dscores",
-    "op3456_attention_fused", "b654_dscores_fused", "b6_dv_fused", "b_column_sums"};
+    "op3456_attention_fused", "b654_dscores_fused", "b6_dv_fused", "b_column_sums", "b6543_attention_packed"};
 
 char* act_ptr(const Ctx& cx, int i) {
   if (i == 0) return const_cast<char*>(static_cast<const char*>(cx.L->x));
@@ -546,11 +564,61 @@ lynx_status run_fused_gelu(Ctx& cx, const FusedGelu& plan, bool keep_u) {
                                             keep_u ? act_ptr(cx, 10) : nullptr, act_ptr(cx, 11)));
 }
 
-// Operators 3-6 as one launch (attn_fused.hip): C and its row statistics from QKV.
+// ---- attention over packed sequences (LYNX_FLAG_PACKED_ATTENTION) ---------------
+// As many sequences as a layer takes: a batch element each, and one per 16 tokens beyond that.
+int most_sequences(const Dims& D) { return D.b + D.T / 16; }
+// Its call's arguments; the pointers come from the caller, as do those that only the backward pass has.
+lynx_attention_config packed_config(const lynx_layer_s* L) {
+  const Dims& D = L->D;
+  lynx_attention_config c{};
+  c.dtype = D.dtype;
+  c.heads = c.kv_heads = D.a;
+  c.head_dim = D.d;
+  c.tokens = D.T;
+  c.sequences = L->sequences;
+  c.scale = 1.0f / sqrtf(static_cast<float>(D.d));
+  c.num_buckets = L->bias.buckets;
+  c.bucket_starts = L->bias.starts;
+  c.q_stride = c.k_stride = c.v_stride = c.dq_stride = c.dk_stride = c.dv_stride = 3ll * D.p;
+  c.out_stride = D.p;
+  return c;
+}
+// Workspace of its backward pass for any sequences and any bias that the layer takes.
+size_t packed_backward_bytes(const Dims& D) {
+  const size_t stats = Arena::round_up(static_cast<size_t>(D.a) * D.T * sizeof(float));
+  const size_t slots = static_cast<size_t>(D.T) / 32 + most_sequences(D);
+  return 2 * stats + Arena::round_up(slots * D.a * LYNX_MAX_BUCKETS * sizeof(float));
+}
+hipError_t packed_forward(const lynx_layer_s* L, const char* qkv, char* c, float* lse, hipStream_t st) {
+  const Dims& D = L->D;
+  const lynx_attention_config cfg = packed_config(L);
+  const size_t col = static_cast<size_t>(D.p) * D.e;
+  // (rows of no sequence: the products after this one read them)
+  const hipError_t e = lynx::attn_packed_clear(D.dtype, c, D.p, D.T, L->offsets, L->sequences, st);
+  if (e != hipSuccess) return e;
+  const lynx_status s = lynx_attention_forward(&cfg, qkv, qkv + col, qkv + 2 * col, L->offsets, L->bias.table, c, lse, st);
+  return s == LYNX_OK ? hipSuccess : hipErrorInvalidValue;
+}
+hipError_t packed_backward(const lynx_layer_s* L, const char* qkv, const char* c, const float* lse, const char* dc, char* dqkv, char* scratch, hipStream_t st) {
+  const Dims& D = L->D;
+  const lynx_attention_config cfg = packed_config(L);
+  const size_t col = static_cast<size_t>(D.p) * D.e;
+  const hipError_t e = lynx::attn_packed_clear(D.dtype, dqkv, 3 * D.p, D.T, L->offsets, L->sequences, st);
+  if (e != hipSuccess) return e;
+  const lynx_status s = lynx_attention_backward(&cfg, qkv, qkv + col, qkv + 2 * col, L->offsets, L->bias.table, c, lse, dc, dqkv, dqkv + col,
+                                                dqkv + 2 * col, L->bias.d_table, scratch, packed_backward_bytes(D), st);
+  return s == LYNX_OK ? hipSuccess : hipErrorInvalidValue;
+}
+
+// Operators 3-6 as one launch (attn_fused.hip, or packed): C and its row statistics from QKV.
 lynx_status run_fused_attention(Ctx& cx) {
   lynx_layer_s* L = cx.L;
   const Dims& D = L->D;
   LYNX_TRY(alloc_act(cx, 6));
+  if (D.packed) {
+    LYNX_LAUNCH(cx, kOp36Fused, packed_forward(L, act_ptr(cx, 2), act_ptr(cx, 6), attn_stats_ptr(cx), cx.st));
+    return LYNX_OK;
+  }
   LYNX_LAUNCH(cx, kOp36Fused, lynx::attn_fused_fwd(act_ptr(cx, 2), 3 * D.p, act_ptr(cx, 6), D.p, attn_stats_ptr(cx),
                                           attn_shape(L), D.d, 1.0f / sqrtf(static_cast<float>(D.d)),
                                           dropout_params(L), cx.st));
@@ -581,9 +649,10 @@ lynx_status run_fused_scores(Ctx& cx, bool write_p, bool with_pd) {
 lynx_status forward_pass(Ctx& cx, uint32_t retain) {
   Book& bk = *cx.bk;
   bk.retain = (retain & 0x3FFFu) | kCallerOwned;
+  if (cx.L->D.packed) bk.retain &= ~0x38u;  // (S, P and Pd do not exist)
   bk.live[0] = true;
-  bk.fused_attn = (cx.L->cfg.flags & LYNX_FLAG_FUSED_ATTENTION) && !(bk.retain & 0x38u) &&
-                  lynx::attn_fused_supported(cx.L->D.dtype, cx.L->D.s, cx.L->D.d);
+  bk.fused_attn = cx.L->D.packed || ((cx.L->cfg.flags & LYNX_FLAG_FUSED_ATTENTION) && !(bk.retain & 0x38u) &&
+                  lynx::attn_fused_supported(cx.L->D.dtype, cx.L->D.s, cx.L->D.d));
   FusedGelu gelu;
   const bool keep_u = (bk.retain >> 10) & 1u;
   for (int i = 1; i <= kNumOps; ++i) {
@@ -701,6 +770,123 @@ lynx_status recompute_pass(Ctx& cx, uint32_t segment) {
 }
 
 // ---- backward ---------------------------------------------------------------
+// Backward of operators 6 to 3: dQKV (allocated here) from dC (released here).
+lynx_status attention_backward(Ctx& cx, Temp* t_dc, Temp* t_dqkv) {
+  lynx_layer_s* L = cx.L;
+  const Dims& D = L->D;
+  const int dt = D.dtype;
+  const size_t e = D.e;
+  Temp t_dpd;
+  // B6: C = Pd V (C itself is read once more below, for the row dot products)
+  LYNX_TRY(alloc_temp(cx, D.ss * e, &t_dpd));
+  LYNX_TRY(alloc_temp(cx, static_cast<size_t>(D.T) * 3 * D.p * e, t_dqkv));
+  char* dqkv = temp_ptr(cx, *t_dqkv);
+  const char* qkv = act_ptr(cx, 2);
+  // dPd = dC V^T, then B5 + B4: Pd = keep0 P c, P = softmax(S / sqrt(d)).  Where the row-block
+  // kernel applies, the store pass of the product forms dS directly (dPd is never written);
+  // the row dot products sum_j dP_ij P_ij it needs equal sum_dd dC[i, dd] C[i, dd] and come
+  // from a small kernel over dC and C, or, up to a size, are formed in the launch that uses
+  // them (attn_score_gradient_from_c).  Otherwise dPd is stored and dS overwrites it.
+  GemmDesc dpd = attn_outer(temp_ptr(cx, *t_dc), D.p, col_block(qkv, D, 2), 3 * D.p, temp_ptr(cx, t_dpd), D);
+  Temp t_rowdot;  // (a place on every path, whichever kernel runs: the sizes named are those they were)
+  LYNX_TRY(alloc_temp(cx, static_cast<size_t>(D.b) * D.a * D.s * sizeof(float), &t_rowdot));
+  dpd.epi.kind = lynx::kEpiSoftmaxBwd;
+  dpd.epi.aux = act_ptr(cx, 4);
+  dpd.epi.aux_ld = D.s;
+  dpd.epi.rowdot = reinterpret_cast<const float*>(temp_ptr(cx, t_rowdot));
+  dpd.epi.scale = 1.0f / sqrtf(static_cast<float>(D.d));
+  dpd.epi.dp = dropout_params(L);
+  dpd.epi.global_heads = D.a * L->cfg.tp_size;
+  dpd.epi.head0 = L->cfg.tp_rank * D.a;
+  const bool fused_ds = lynx::gemm_supported(dt, dpd);
+  // (elsewhere, up to s = 1024, the dot products are formed from dPd itself, in the launch that forms dPd)
+  const bool rows_ds = !fused_ds && lynx::attn_score_gradient_supported(dt, D.s, D.d, 3ll * D.p, static_cast<long long>(D.b) * D.a);
+  // dV = Pd^T dC.  With the one-pass dS kernels it goes first, so that dQ and dK read dS right
+  // after it is written, while much of it is still in the caches (measured: dQ 0.070 -> 0.05x ms).
+  const bool dv_first = (fused_ds || rows_ds) && !cx.bk->fused_attn;
+  const GemmDesc dv = attn_cols(act_ptr(cx, 5), temp_ptr(cx, *t_dc), D.p, const_cast<char*>(col_block(dqkv, D, 2)), 3 * D.p, D);
+  const bool dpd_with_dv = dt == LYNX_F32;  // one launch
+  auto launch_dv = [&]() -> lynx_status {
+    LYNX_LAUNCH(cx, kB6DV, lynx::gemm(dt, dv, nullptr, 0, cx.st));
+    return LYNX_OK;
+  };
+  if (dv_first) {
+    LYNX_TRY(launch_dv());
+    free_act(cx, 5);
+  }
+  if (cx.bk->fused_attn) {
+    // neither P nor Pd exists: both kernels rebuild them from QKV and the row statistics of C
+    float* rowdot = reinterpret_cast<float*>(temp_ptr(cx, t_rowdot));
+    LYNX_LAUNCH(cx, kB6RowDot, lynx::attn_rowdot(dt, temp_ptr(cx, *t_dc), act_ptr(cx, 6), rowdot, D.b, D.a, D.s, D.d,
+                                                 D.p, cx.st));
+    LYNX_LAUNCH(cx, kB654DScoresFused, lynx::attn_fused_bwd_ds(qkv, 3 * D.p, temp_ptr(cx, *t_dc), D.p, attn_stats_ptr(cx),
+                                                          rowdot, temp_ptr(cx, t_dpd), attn_shape(L), D.d,
+                                                          dpd.epi.scale, dropout_params(L), cx.st));
+  } else if (fused_ds && lynx::attn_score_gradient_from_c(dt, D.s, D.d, 3ll * D.p, static_cast<long long>(D.b) * D.a)) {
+    LYNX_LAUNCH(cx, kB654DScores, lynx::attn_score_gradient(temp_ptr(cx, *t_dc), D.p, col_block(qkv, D, 2), 3ll * D.p, act_ptr(cx, 6),
+                                                            act_ptr(cx, 4), temp_ptr(cx, t_dpd), attn_shape(L), D.d,
+                                                            dpd.epi.scale, dropout_params(L), cx.st));
+  } else if (fused_ds) {
+    LYNX_LAUNCH(cx, kB6RowDot, lynx::attn_rowdot(dt, temp_ptr(cx, *t_dc), act_ptr(cx, 6),
+                                                 reinterpret_cast<float*>(temp_ptr(cx, t_rowdot)), D.b, D.a, D.s,
+                                                 D.d, D.p, cx.st));
+    LYNX_LAUNCH(cx, kB654DScores, lynx::gemm(dt, dpd, nullptr, 0, cx.st));
+  } else if (rows_ds) {
+    LYNX_LAUNCH(cx, kB654DScores, lynx::attn_score_gradient(temp_ptr(cx, *t_dc), D.p, col_block(qkv, D, 2), 3ll * D.p, nullptr,
+                                                            act_ptr(cx, 4), temp_ptr(cx, t_dpd), attn_shape(L), D.d,
+                                                            dpd.epi.scale, dropout_params(L), cx.st));
+  } else {
+    dpd.epi = lynx::GemmEpilogue{};
+    if (dpd_with_dv) {
+      LYNX_LAUNCH(cx, kB6DPd, lynx::gemm_seq_pair(dt, dpd, dv, cx.st));
+    } else {
+      LYNX_LAUNCH(cx, kB6DPd, lynx::gemm(dt, dpd, nullptr, 0, cx.st));
+    }
+  }
+  free_temp(cx, &t_rowdot);
+  if (cx.bk->fused_attn) {
+    LYNX_LAUNCH(cx, kB6DVFused, lynx::attn_fused_bwd_dv(qkv, 3 * D.p, temp_ptr(cx, *t_dc), D.p, attn_stats_ptr(cx), dqkv,
+                                                   3 * D.p, attn_shape(L), D.d, 1.0f / sqrtf(static_cast<float>(D.d)),
+                                                   dropout_params(L), cx.st));
+  } else if (!dv_first && !dpd_with_dv) {
+    LYNX_TRY(launch_dv());
+  }
+  free_temp(cx, t_dc);
+  free_act(cx, 5);
+  free_act(cx, 6);
+  if (!fused_ds && !rows_ds && !cx.bk->fused_attn) {
+    LYNX_LAUNCH(cx, kB54Softmax, lynx::softmax_dropout_bwd(dt, temp_ptr(cx, t_dpd), act_ptr(cx, 4),
+                                              temp_ptr(cx, t_dpd), attn_shape(L),
+                                              1.0f / sqrtf(static_cast<float>(D.d)), dropout_params(L),
+                                              cx.st));
+  }
+  free_act(cx, 4);
+  LYNX_TRY(tap(cx, 3, temp_ptr(cx, t_dpd)));
+  // B3: S = Q K^T
+  const GemmDesc dq = attn_rows(temp_ptr(cx, t_dpd), col_block(qkv, D, 1), 3 * D.p,
+                                const_cast<char*>(col_block(dqkv, D, 0)), 3 * D.p, D);
+  const GemmDesc dk = attn_cols(temp_ptr(cx, t_dpd), col_block(qkv, D, 0), 3 * D.p,
+                                const_cast<char*>(col_block(dqkv, D, 1)), 3 * D.p, D);
+  LYNX_LAUNCH(cx, kB3DQ, lynx::gemm_seq_pair(dt, dq, dk, cx.st));
+  free_temp(cx, &t_dpd);
+  free_act(cx, 3);
+  return LYNX_OK;
+}
+// The same of packed sequences: no seq x seq gradient either.
+lynx_status packed_attention_backward(Ctx& cx, Temp* t_dc, Temp* t_dqkv) {
+  lynx_layer_s* L = cx.L;
+  const Dims& D = L->D;
+  Temp scratch;
+  LYNX_TRY(alloc_temp(cx, packed_backward_bytes(D), &scratch));
+  LYNX_TRY(alloc_temp(cx, static_cast<size_t>(D.T) * 3 * D.p * D.e, t_dqkv));
+  LYNX_LAUNCH(cx, kB6543Packed, packed_backward(L, act_ptr(cx, 2), act_ptr(cx, 6), attn_stats_ptr(cx), temp_ptr(cx, *t_dc), temp_ptr(cx, *t_dqkv),
+                                                temp_ptr(cx, scratch), cx.st));
+  free_temp(cx, &scratch);
+  free_temp(cx, t_dc);
+  free_act(cx, 6);
+  return LYNX_OK;
+}
+
 lynx_status backward_pass(Ctx& cx, const void* d_out, void* d_x, const lynx_grads* gr) {
   lynx_layer_s* L = cx.L;
   const Dims& D = L->D;
@@ -733,7 +919,7 @@ lynx_status backward_pass(Ctx& cx, const void* d_out, void* d_x, const lynx_grad
         if (b > scratch_bytes) scratch_bytes = b;
       }
   }
-  Temp scratch, t_dv2, t_du, t_dy2, t_dx2, t_do, t_dc, t_dpd, t_dqkv, t_dy1;
+  Temp scratch, t_dv2, t_du, t_dy2, t_dx2, t_do, t_dc, t_dqkv, t_dy1;
   LYNX_TRY(alloc_temp(cx, scratch_bytes, &scratch, without(*cx.bk, kScratchHigh)));
   float* scr = reinterpret_cast<float*>(temp_ptr(cx, scratch));
   const bool early_high = without(*cx.bk, kEarlyHigh);
@@ -826,99 +1012,9 @@ lynx_status backward_pass(Ctx& cx, const void* d_out, void* d_x, const lynx_grad
                        linear_wgrad(temp_ptr(cx, t_do), act_ptr(cx, 6), gr->wo, D.T, D.h, D.p), defer));
   free_temp(cx, &t_do);
   LYNX_TRY(tap(cx, 6, temp_ptr(cx, t_dc)));
-  // B6: C = Pd V (C itself is read once more below, for the row dot products)
-  LYNX_TRY(alloc_temp(cx, D.ss * e, &t_dpd));
-  LYNX_TRY(alloc_temp(cx, static_cast<size_t>(D.T) * 3 * D.p * e, &t_dqkv));
-  char* dqkv = temp_ptr(cx, t_dqkv);
-  const char* qkv = act_ptr(cx, 2);
-  // dPd = dC V^T, then B5 + B4: Pd = keep0 P c, P = softmax(S / sqrt(d)).  Where the row-block
-  // kernel applies, the store pass of the product forms dS directly (dPd is never written);
-  // the row dot products sum_j dP_ij P_ij it needs equal sum_dd dC[i, dd] C[i, dd] and come
-  // from a small kernel over dC and C, or, up to a size, are formed in the launch that uses
-  // them (attn_score_gradient_from_c).  Otherwise dPd is stored and dS overwrites it.
-  GemmDesc dpd = attn_outer(temp_ptr(cx, t_dc), D.p, col_block(qkv, D, 2), 3 * D.p, temp_ptr(cx, t_dpd), D);
-  Temp t_rowdot;  // (a place on every path, whichever kernel runs: the sizes named are those they were)
-  LYNX_TRY(alloc_temp(cx, static_cast<size_t>(D.b) * D.a * D.s * sizeof(float), &t_rowdot));
-  dpd.epi.kind = lynx::kEpiSoftmaxBwd;
-  dpd.epi.aux = act_ptr(cx, 4);
-  dpd.epi.aux_ld = D.s;
-  dpd.epi.rowdot = reinterpret_cast<const float*>(temp_ptr(cx, t_rowdot));
-  dpd.epi.scale = 1.0f / sqrtf(static_cast<float>(D.d));
-  dpd.epi.dp = dropout_params(L);
-  dpd.epi.global_heads = D.a * L->cfg.tp_size;
-  dpd.epi.head0 = L->cfg.tp_rank * D.a;
-  const bool fused_ds = lynx::gemm_supported(dt, dpd);
-  // (elsewhere, up to s = 1024, the dot products are formed from dPd itself, in the launch that forms dPd)
-  const bool rows_ds = !fused_ds && lynx::attn_score_gradient_supported(dt, D.s, D.d, 3ll * D.p, static_cast<long long>(D.b) * D.a);
-  // dV = Pd^T dC.  With the one-pass dS kernels it goes first, so that dQ and dK read dS right
-  // after it is written, while much of it is still in the caches (measured: dQ 0.070 -> 0.05x ms).
-  const bool dv_first = (fused_ds || rows_ds) && !cx.bk->fused_attn;
-  const GemmDesc dv = attn_cols(act_ptr(cx, 5), temp_ptr(cx, t_dc), D.p, const_cast<char*>(col_block(dqkv, D, 2)), 3 * D.p, D);
-  const bool dpd_with_dv = dt == LYNX_F32;  // one launch
-  auto launch_dv = [&]() -> lynx_status {
-    LYNX_LAUNCH(cx, kB6DV, lynx::gemm(dt, dv, nullptr, 0, cx.st));
-    return LYNX_OK;
-  };
-  if (dv_first) {
-    LYNX_TRY(launch_dv());
-    free_act(cx, 5);
-  }
-  if (cx.bk->fused_attn) {
-    // neither P nor Pd exists: both kernels rebuild them from QKV and the row statistics of C
-    float* rowdot = reinterpret_cast<float*>(temp_ptr(cx, t_rowdot));
-    LYNX_LAUNCH(cx, kB6RowDot, lynx::attn_rowdot(dt, temp_ptr(cx, t_dc), act_ptr(cx, 6), rowdot, D.b, D.a, D.s, D.d,
-                                                 D.p, cx.st));
-    LYNX_LAUNCH(cx, kB654DScoresFused, lynx::attn_fused_bwd_ds(qkv, 3 * D.p, temp_ptr(cx, t_dc), D.p, attn_stats_ptr(cx),
-                                                          rowdot, temp_ptr(cx, t_dpd), attn_shape(L), D.d,
-                                                          dpd.epi.scale, dropout_params(L), cx.st));
-  } else if (fused_ds && lynx::attn_score_gradient_from_c(dt, D.s, D.d, 3ll * D.p, static_cast<long long>(D.b) * D.a)) {
-    LYNX_LAUNCH(cx, kB654DScores, lynx::attn_score_gradient(temp_ptr(cx, t_dc), D.p, col_block(qkv, D, 2), 3ll * D.p, act_ptr(cx, 6),
-                                                            act_ptr(cx, 4), temp_ptr(cx, t_dpd), attn_shape(L), D.d,
-                                                            dpd.epi.scale, dropout_params(L), cx.st));
-  } else if (fused_ds) {
-    LYNX_LAUNCH(cx, kB6RowDot, lynx::attn_rowdot(dt, temp_ptr(cx, t_dc), act_ptr(cx, 6),
-                                                 reinterpret_cast<float*>(temp_ptr(cx, t_rowdot)), D.b, D.a, D.s,
-                                                 D.d, D.p, cx.st));
-    LYNX_LAUNCH(cx, kB654DScores, lynx::gemm(dt, dpd, nullptr, 0, cx.st));
-  } else if (rows_ds) {
-    LYNX_LAUNCH(cx, kB654DScores, lynx::attn_score_gradient(temp_ptr(cx, t_dc), D.p, col_block(qkv, D, 2), 3ll * D.p, nullptr,
-                                                            act_ptr(cx, 4), temp_ptr(cx, t_dpd), attn_shape(L), D.d,
-                                                            dpd.epi.scale, dropout_params(L), cx.st));
-  } else {
-    dpd.epi = lynx::GemmEpilogue{};
-    if (dpd_with_dv) {
-      LYNX_LAUNCH(cx, kB6DPd, lynx::gemm_seq_pair(dt, dpd, dv, cx.st));
-    } else {
-      LYNX_LAUNCH(cx, kB6DPd, lynx::gemm(dt, dpd, nullptr, 0, cx.st));
-    }
-  }
-  free_temp(cx, &t_rowdot);
-  if (cx.bk->fused_attn) {
-    LYNX_LAUNCH(cx, kB6DVFused, lynx::attn_fused_bwd_dv(qkv, 3 * D.p, temp_ptr(cx, t_dc), D.p, attn_stats_ptr(cx), dqkv,
-                                                   3 * D.p, attn_shape(L), D.d, 1.0f / sqrtf(static_cast<float>(D.d)),
-                                                   dropout_params(L), cx.st));
-  } else if (!dv_first && !dpd_with_dv) {
-    LYNX_TRY(launch_dv());
-  }
-  free_temp(cx, &t_dc);
-  free_act(cx, 5);
-  free_act(cx, 6);
-  if (!fused_ds && !rows_ds && !cx.bk->fused_attn) {
-    LYNX_LAUNCH(cx, kB54Softmax, lynx::softmax_dropout_bwd(dt, temp_ptr(cx, t_dpd), act_ptr(cx, 4),
-                                              temp_ptr(cx, t_dpd), attn_shape(L),
-                                              1.0f / sqrtf(static_cast<float>(D.d)), dropout_params(L),
-                                              cx.st));
-  }
-  free_act(cx, 4);
-  LYNX_TRY(tap(cx, 3, temp_ptr(cx, t_dpd)));
-  // B3: S = Q K^T
-  const GemmDesc dq = attn_rows(temp_ptr(cx, t_dpd), col_block(qkv, D, 1), 3 * D.p,
-                                const_cast<char*>(col_block(dqkv, D, 0)), 3 * D.p, D);
-  const GemmDesc dk = attn_cols(temp_ptr(cx, t_dpd), col_block(qkv, D, 0), 3 * D.p,
-                                const_cast<char*>(col_block(dqkv, D, 1)), 3 * D.p, D);
-  LYNX_LAUNCH(cx, kB3DQ, lynx::gemm_seq_pair(dt, dq, dk, cx.st));
-  free_temp(cx, &t_dpd);
-  free_act(cx, 3);
+  // B6 to B3: the attention operators, dQKV from dC
+  LYNX_TRY(D.packed ? packed_attention_backward(cx, &t_dc, &t_dqkv) : attention_backward(cx, &t_dc, &t_dqkv));
+  const char* dqkv = temp_ptr(cx, t_dqkv);
   LYNX_TRY(tap(cx, 2, dqkv));
   // B2: QKV = Y1 Wqkv^T + bqkv
   LYNX_TRY(alloc_temp(cx, th, &t_dy1));
@@ -1126,6 +1222,42 @@ lynx_status lynx_layer_set_params(lynx_layer_t L, const lynx_params* params) {
   return LYNX_OK;
 }
 
+lynx_status lynx_layer_set_sequences(lynx_layer_t L, const int32_t* offsets, int32_t sequences) {
+  if (L == nullptr || offsets == nullptr || (reinterpret_cast<uintptr_t>(offsets) & 3u)) return LYNX_ERR_INVALID_ARG;
+  if (!L->D.packed || L->book.state != 0) return LYNX_ERR_STATE;
+  if (sequences <= 0 || sequences > most_sequences(L->D)) return LYNX_ERR_SHAPE;
+  lynx_attention_config c = packed_config(L);  // (what the kernels' own call would refuse)
+  c.sequences = sequences;
+  const lynx_status s = lynx::attention_check(&c);
+  if (s != LYNX_OK) return s;
+  L->offsets = offsets;
+  L->sequences = sequences;
+  return LYNX_OK;
+}
+
+lynx_status lynx_layer_set_position_bias(lynx_layer_t L, int32_t num_buckets, const int32_t* bucket_starts, const void* table,
+                                         void* d_table) {
+  if (L == nullptr || num_buckets < 0) return LYNX_ERR_INVALID_ARG;
+  if (!L->D.packed || L->book.state != 0) return LYNX_ERR_STATE;
+  if (num_buckets == 0) {
+    L->bias.buckets = 0;
+    return LYNX_OK;
+  }
+  if (num_buckets > LYNX_MAX_BUCKETS) return LYNX_ERR_SHAPE;
+  if (bucket_starts == nullptr || !aligned16(table) || !aligned16(d_table)) return LYNX_ERR_INVALID_ARG;
+  lynx_attention_config c = packed_config(L);
+  c.num_buckets = num_buckets;
+  c.bucket_starts = bucket_starts;
+  c.sequences = most_sequences(L->D);
+  const lynx_status s = lynx::attention_check(&c);
+  if (s != LYNX_OK) return s;
+  L->bias.buckets = num_buckets;
+  memcpy(L->bias.starts, bucket_starts, num_buckets * sizeof(int32_t));
+  L->bias.table = table;
+  L->bias.d_table = d_table;
+  return LYNX_OK;
+}
+
 lynx_status lynx_layer_set_dry_run(lynx_layer_t L, int on) {
   if (L == nullptr) return LYNX_ERR_INVALID_ARG;
   L->dry = on != 0;
@@ -1137,6 +1269,7 @@ lynx_status lynx_layer_forward(lynx_layer_t L, const void* x, void* out, uint32_
   if (L == nullptr || !aligned16(x) || !aligned16(out)) return LYNX_ERR_INVALID_ARG;
   if (retain_mask & ~0x3FFFu) return LYNX_ERR_INVALID_ARG;
   if (step >> 32) return LYNX_ERR_INVALID_ARG;
+  if (L->D.packed && L->offsets == nullptr && !L->dry) return LYNX_ERR_STATE;
   if (!L->have_params || L->book.state != 0) return LYNX_ERR_STATE;
   const void* old_x = L->x;
   void* old_out = L->out;
@@ -1247,7 +1380,7 @@ lynx_status lynx_dropout_mask(const lynx_layer_config* cfg, uint64_t step, int s
 }
 
 lynx_status lynx_layer_set_gradient_tap(lynx_layer_t L, int act_id, void* device_dst) {
-  if (L == nullptr || act_id < 0 || act_id >= kNumAct || !((kTappable >> act_id) & 1u))
+  if (L == nullptr || act_id < 0 || act_id >= kNumAct || !((kTappable >> act_id) & 1u) || (L->D.packed && act_id == 3))
     return LYNX_ERR_INVALID_ARG;
   if (device_dst != nullptr && !aligned16(device_dst)) return LYNX_ERR_INVALID_ARG;
   L->grad_tap[act_id] = device_dst;
@@ -1302,13 +1435,14 @@ lynx_status lynx_policy_layer_problem(const lynx_layer_config* cfg, lynx_policy_
   for (int i = 1; i <= kNumOps; ++i) {
     uint32_t m = 0;
     for (int k = 0; k < 3 && kParents[i][k] >= 0; ++k) m |= 1u << kParents[i][k];
+    if (D.packed && i == 6) m = 1u << 2;  // (operators 3 to 5 do not exist: no bytes, and nobody's input)
     parents_out[i - 1] = m;
     bytes_out[i - 1] = static_cast<double>(act_bytes(D, i));
   }
   problem_out->n_ops = kNumOps;
   problem_out->parents = parents_out;
   problem_out->bytes = bytes_out;
-  problem_out->needed_mask = kBackwardNeeds;
+  problem_out->needed_mask = D.packed ? kBackwardNeeds & ~0x30u : kBackwardNeeds;
   problem_out->comm_mask = 0;
   return LYNX_OK;
 }

@@ -1,0 +1,124 @@
+"""Layers of packed sequences on the host: sizes, the order of calls, refusals and the policy problem, without a GPU."""
+import ctypes as C
+
+import pytest
+
+import lynx_synth as synth
+
+B = pytest.importorskip("paper_2406_08756_amd.binding")
+
+CFG = synth.LayerConfig(synth.BF16, 64, 2, 40, 64, 72, 2, tp_size=2, flags=B.LYNX_FLAG_PACKED_ATTENTION)
+FAKE = 4096
+
+
+def layer(cfg=CFG, mask=B.LYNX_RETAIN_STORE_ALL):
+    h = B.lynx_layer_create(cfg, FAKE, B.lynx_workspace_bytes(cfg, mask))
+    B.lynx_layer_set_params(h, {n: FAKE for n in B.PARAM_FIELDS})
+    return h
+
+
+def status(call, *a):
+    with pytest.raises(B.LynxError) as e:
+        call(*a)
+    return e.value.status
+
+
+def test_no_seq_by_seq_activation():
+    assert [B.lynx_activation_bytes(CFG, i) for i in (3, 4, 5)] == [0, 0, 0]
+    plain = CFG.with_(flags=0)
+    for i in (1, 2, 6, 8, 9, 10, 11):
+        assert B.lynx_activation_bytes(CFG, i) == B.lynx_activation_bytes(plain, i) > 0
+    long = CFG.with_(seq=8192, micro_batch=1)
+    assert B.lynx_workspace_bytes(long, B.LYNX_RETAIN_STORE_ALL) < B.lynx_workspace_bytes(long.with_(flags=0), B.LYNX_RETAIN_STORE_ALL) / 4
+
+
+@pytest.mark.parametrize("cfg", [CFG.with_(flags=3), CFG.with_(flags=4), CFG.with_(head_dim=136)], ids=["fused", "flag", "head_dim"])
+def test_refused_configs(cfg):
+    assert B.lynx_workspace_bytes(cfg, 1) == 0
+    assert status(B.lynx_layer_create, cfg, FAKE, 1 << 30) == B.LYNX_ERR_SHAPE
+
+
+@pytest.mark.parametrize("mask", [B.LYNX_RETAIN_STORE_ALL, B.LYNX_RETAIN_FULL_RECOMPUTE, B.LYNX_RETAIN_ATTENTION_ONLY, 0x2841])
+def test_bookkeeping(mask):
+    h = layer(mask=mask)
+    B.lynx_layer_set_dry_run(h, True)
+    B.lynx_layer_forward(h, FAKE, FAKE, mask)
+    live = B.lynx_layer_live_mask(h)
+    assert live == (mask | 0x2001) & ~0x38
+    assert B.lynx_layer_live_bytes(h) == sum(B.lynx_activation_bytes(CFG, i) for i in range(1, 13) if live >> i & 1)
+    assert B.lynx_layer_missing_mask(h) & 0x38 == 0
+    B.lynx_recompute(h, 0x38)  # operators 3 to 5 do not exist: nothing happens
+    assert B.lynx_layer_live_mask(h) == live
+    B.lynx_recompute(h, B.LYNX_SEG_ALL_MISSING)
+    B.lynx_layer_backward(h, FAKE, FAKE, {n: FAKE for n in B.PARAM_FIELDS})
+    assert B.lynx_layer_live_mask(h) == 0
+    assert B.lynx_layer_peak_bytes(h) <= B.lynx_workspace_bytes(CFG, mask)
+    B.lynx_layer_destroy(h)
+
+
+def test_operator_6_reads_qkv_alone():
+    h = layer()
+    B.lynx_layer_set_dry_run(h, True)
+    B.lynx_layer_forward(h, FAKE, FAKE, 0x2001 | 4)
+    B.lynx_recompute(h, 1 << 6)
+    assert B.lynx_layer_live_mask(h) == 0x2001 | 4 | 64
+    B.lynx_layer_reset(h)
+    B.lynx_layer_forward(h, FAKE, FAKE, 0x2001)
+    assert status(B.lynx_recompute, h, 1 << 6) == B.LYNX_ERR_DEPENDENCY
+    B.lynx_layer_destroy(h)
+
+
+def test_order_of_calls_and_refusals():
+    h = layer()
+    assert status(B.lynx_layer_forward, h, FAKE, FAKE, 1) == B.LYNX_ERR_STATE  # no sequences yet: nothing is launched
+    most = CFG.micro_batch + CFG.tokens // 16
+    for n in (0, -1, most + 1):
+        assert status(B.lynx_layer_set_sequences, h, FAKE, n) == B.LYNX_ERR_SHAPE
+    for bad in (None, 4097):
+        assert status(B.lynx_layer_set_sequences, h, bad, 1) == B.LYNX_ERR_INVALID_ARG
+    B.lynx_layer_set_sequences(h, FAKE, most)
+    starts = B.lynx_position_buckets(16, 64)
+    B.lynx_layer_set_position_bias(h, 16, starts, FAKE, FAKE)
+    for a in ((16, None, FAKE, FAKE), (16, starts, None, FAKE), (16, starts, FAKE, 4100), (-1, starts, FAKE, FAKE)):
+        assert status(B.lynx_layer_set_position_bias, h, *a) == B.LYNX_ERR_INVALID_ARG
+    assert status(B.lynx_layer_set_position_bias, h, 65, starts, FAKE, FAKE) == B.LYNX_ERR_SHAPE
+    assert status(B.lynx_layer_set_position_bias, h, 2, (C.c_int32 * 2)(0, 2049), FAKE, FAKE) == B.LYNX_ERR_SHAPE
+    assert status(B.lynx_layer_set_position_bias, h, 2, (C.c_int32 * 2)(1, 2), FAKE, FAKE) == B.LYNX_ERR_INVALID_ARG
+    assert status(B.lynx_layer_set_gradient_tap, h, 3, FAKE) == B.LYNX_ERR_INVALID_ARG
+    B.lynx_layer_set_dry_run(h, True)
+    B.lynx_layer_forward(h, FAKE, FAKE, 1)
+    assert status(B.lynx_layer_set_sequences, h, FAKE, 1) == B.LYNX_ERR_STATE
+    assert status(B.lynx_layer_set_position_bias, h, 0) == B.LYNX_ERR_STATE
+    B.lynx_layer_reset(h)
+    B.lynx_layer_set_position_bias(h, 0)
+    B.lynx_layer_destroy(h)
+    h = layer(CFG.with_(flags=0))
+    assert status(B.lynx_layer_set_sequences, h, FAKE, 1) == B.LYNX_ERR_STATE
+    assert status(B.lynx_layer_set_position_bias, h, 0) == B.LYNX_ERR_STATE
+    B.lynx_layer_destroy(h)
+    assert B._lib.lynx_layer_set_sequences(None, FAKE, 1) == B.LYNX_ERR_INVALID_ARG
+    assert B._lib.lynx_layer_set_position_bias(None, 0, None, None, None) == B.LYNX_ERR_INVALID_ARG
+
+
+def test_the_workspace_takes_any_sequences_and_bias():
+    """The room that backward keeps covers what the kernels' own call asks for."""
+    for seq, b, heads in ((8, 1, 1), (72, 2, 2), (2048, 8, 5), (8192, 4, 3)):
+        cfg = CFG.with_(seq=seq, micro_batch=b, local_heads=heads, head_dim=128)
+        t = cfg.tokens
+        need = 0
+        for n in {1, b + t // 16}:
+            starts = B.lynx_position_buckets(64, 2048)
+            p3 = 3 * cfg.proj
+            c = B.lynx_attention_config(dtype=B.LYNX_BF16, heads=heads, kv_heads=heads, head_dim=128, tokens=t, sequences=n, scale=0.1,
+                                        num_buckets=64, bucket_starts=starts, q_stride=p3, k_stride=p3, v_stride=p3, out_stride=cfg.proj,
+                                        dq_stride=p3, dk_stride=p3, dv_stride=p3)
+            need = max(need, B.lynx_attention_backward_bytes(c))
+        stats = (heads * t * 4 + 255) // 256 * 256
+        assert need <= 2 * stats + ((t // 32 + b + t // 16) * heads * 64 * 4 + 255) // 256 * 256
+
+
+def test_policy_problem():
+    p = B.lynx_policy_layer_problem(CFG, [1.0] * 13, [0.0] * 4, 1e9)
+    assert p["parents"][5] == (2,)
+    assert not p["needed"] & {4, 5}
+    assert [p["bytes"][i] for i in (2, 3, 4)] == [0.0, 0.0, 0.0]
