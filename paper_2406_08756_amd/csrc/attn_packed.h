@@ -78,10 +78,13 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int til
   while (true) {
     const int per = (count + kWave - 1) / kWave;
     int sum = 0;
+    int2 span = make_int2(0, 0);
     for (int i = 0; i < per; ++i) {
       const int s = lane * per + i;
+      if (s >= count) continue;
+      span = sequence_span(g, first + s);
       // (the limit: offsets that fall name rows many times, and their sum must not pass 32 bits)
-      if (s < count) sum = min(sum + (((sequence_span(g, first + s).y << pack) + (1 << tile_log) - 1) >> tile_log), kMostTiles);
+      sum = min(sum + (((span.y << pack) + (1 << tile_log) - 1) >> tile_log), kMostTiles);
     }
     int upto = sum;
 #pragma unroll
@@ -97,15 +100,15 @@ __device__ __forceinline__ bool find_tile(const PackedAttn& g, int slot, int til
     }
     const int at = __builtin_ctzll(__ballot(upto > target));
     target -= __builtin_amdgcn_readlane(upto - sum, at);
+    if (per == 1) {
+      out->start = __builtin_amdgcn_readlane(span.x, at);
+      out->len = __builtin_amdgcn_readlane(span.y, at);
+      out->tile = __builtin_amdgcn_readfirstlane(target);
+      return true;
+    }
     first += at * per;
     count = min(per, count - at * per);
-    if (per == 1) break;
   }
-  const int2 span = sequence_span(g, first);
-  out->start = __builtin_amdgcn_readfirstlane(span.x);
-  out->len = __builtin_amdgcn_readfirstlane(span.y);
-  out->tile = __builtin_amdgcn_readfirstlane(target);
-  return true;
 }
 
 // The same, the tiles with the most to see first over all sequences: a tile's size is its number, counted from the end that
@@ -117,10 +120,12 @@ __device__ __forceinline__ bool find_ranked_tile(const PackedAttn& g, int slot, 
   if (g.sequences > kRankedSequences) return find_tile<true>(g, slot, tile_log, pack, out);
   const int lane = threadIdx.x & (kWave - 1);
   int tiles[2];
+  int2 span[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int s = k * kWave + lane;
-    tiles[k] = s < g.sequences ? ((sequence_span(g, s).y << pack) + (1 << tile_log) - 1) >> tile_log : 0;
+    span[k] = s < g.sequences ? sequence_span(g, s) : make_int2(0, 0);
+    tiles[k] = ((span[k].y << pack) + (1 << tile_log) - 1) >> tile_log;
   }
   // how many tiles have a number of `from` or more: falls with `from`; each lane counts for one number
   const auto count = [&](int from) {
@@ -146,20 +151,19 @@ __device__ __forceinline__ bool find_ranked_tile(const PackedAttn& g, int slot, 
     lo += last * step;
     range = step;
   }
-  int rank = slot - above, at = 0;  // among the sequences that have a tile of that number
+  int rank = slot - above;  // among the sequences that have a tile of that number
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     unsigned long long has = __ballot(tiles[k] > lo);
     const int n = __builtin_popcountll(has);
     if (rank >= 0 && rank < n) {
       for (int i = 0; i < rank; ++i) has &= has - 1;
-      at = k * kWave + __builtin_ctzll(has);
+      const int at = __builtin_ctzll(has);
+      out->start = __builtin_amdgcn_readlane(span[k].x, at);
+      out->len = __builtin_amdgcn_readlane(span[k].y, at);
     }
     rank -= n;
   }
-  const int2 span = sequence_span(g, at);
-  out->start = __builtin_amdgcn_readfirstlane(span.x);
-  out->len = __builtin_amdgcn_readfirstlane(span.y);
   out->tile = lo;
   return true;
 }

@@ -69,7 +69,7 @@ __device__ void sum_row_dq(const PackedAttn& g, const T* q, const T* d_out, cons
 }
 
 template <typename T, int DP, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void attn_packed_rows_kernel(PackedAttn g) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 || (DP == 64 && !SPLIT) ? 2 : 1) void attn_packed_rows_kernel(PackedAttn g) {
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
   typedef Rows<T, DP, BIAS, SPLIT> S;
@@ -91,11 +91,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
         g.partials[(static_cast<long long>(slot) * g.heads + head0) * g.buckets + x] = 0.f;
     return;
   }
-  if (BIAS) {
-    fill_bias<T, kThreads>(g, head0, bias);
-    for (int x = threadIdx.x; x < kWaves * by_distance_floats(g); x += kThreads) sums[x] = 0.f;
-  }
-
   const int kv = head0 / (g.heads / g.kv_heads);
   const T* const q = static_cast<const T*>(g.q) + w.start * g.q_stride + static_cast<long long>(head0) * g.d;
   const T* const k = static_cast<const T*>(g.k) + w.start * g.k_stride + static_cast<long long>(kv) * g.d;
@@ -110,6 +105,27 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
   const bool there = tok < w.len;
   const float scale2 = g.scale * kLog2e;
 
+  constexpr int kTogether = SPLIT ? kWave : kThreads;
+  typedef Stream<T, DP, kTogether> Load;
+  const int part = SPLIT ? 0 : wave;  // of a tile's load
+  const uint32_t lds_at = lds_address(smem_raw);
+  // SPLIT: the wavefronts deal the tiles up to the last one that the rows see; else the workgroup's rows see these
+  const int end_tok = SPLIT ? last_tok + 1 : min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);
+  const int tiles = (end_tok + 31) / 32;
+  const int first_tile = SPLIT ? wave : 0, every = SPLIT ? kWaves : 1;
+  constexpr int kKs = SPLIT ? 1 : S::kFew ? 3 : 4, kVs = SPLIT ? 1 : S::kFew ? 2 : 4;
+  const auto k_slot = [&](int t) { return (SPLIT ? 2 * wave : t % kKs) * kTileElems; };
+  const auto v_slot = [&](int t) { return (SPLIT ? 2 * wave + 1 : kKs + t % kVs) * kTileElems; };
+  Load k_tiles(k, g.k_stride, 32 * first_tile, w.len, g.d, 0, part, lane), v_tiles(v, g.v_stride, 32 * first_tile, w.len, g.d, 0, part, lane);
+  const auto load = [&](int kt, int vt) {  // (each in turn)
+    if (kt < tiles) k_tiles.load(lds_at + k_slot(kt) * sizeof(T), part, every);
+    if (vt < tiles) v_tiles.load(lds_at + v_slot(vt) * sizeof(T), part, every);
+  };
+  const auto load_first = [&] {
+    load(first_tile, first_tile);
+    if (!SPLIT && !S::kFew) load(1, 1);
+  };
+
   typename Op::Frag qf[L::kSteps], gf[L::kSteps];  // Q and d_out
   float delta = 0.f, lse2 = kInf;
   {
@@ -120,27 +136,28 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
     const auto at = [&](long long stride) {
       return (static_cast<uint32_t>(tok - first_tok) * static_cast<uint32_t>(stride) + hp * g.d) * static_cast<uint32_t>(sizeof(T));
     };
-    load_row_frags<T, DP>(buffer(out, g.out_stride), at(g.out_stride), g.d, lane, qf);
+    // all loads on their way before the first is waited for, the first tiles' and the bias's too
+    typename Op::Frag of[L::kSteps];
+    load_row_frags<T, DP>(buffer(out, g.out_stride), at(g.out_stride), g.d, lane, of);
     load_row_frags<T, DP>(buffer(d_out, g.out_stride), at(g.out_stride), g.d, lane, gf);
-#pragma unroll
-    for (int s = 0; s < L::kSteps; ++s) delta += Op::dot(qf[s], gf[s]);
-    delta = sum_of_halves(delta);
     load_row_frags<T, DP>(buffer(q, g.q_stride), at(g.q_stride), g.d, lane, qf);
-    if (there) {
-      const long long stat = static_cast<long long>(head0 + hp) * g.tokens + w.start + tok;
-      lse2 = offset2(g.lse[stat]);
+    float lse = -kInf;
+    if (there) lse = g.lse[static_cast<long long>(head0 + hp) * g.tokens + w.start + tok];
+    load_first();
+    if (BIAS) {
+      fill_bias<T, kThreads>(g, head0, bias);
+      for (int x = threadIdx.x; x < kWaves * by_distance_floats(g); x += kThreads) sums[x] = 0.f;
     }
+#pragma unroll
+    for (int s = 0; s < L::kSteps; ++s) delta += Op::dot(of[s], gf[s]);
+    delta = sum_of_halves(delta);
+    lse2 = offset2(lse);
   }
   const float* const my_bias = BIAS ? bias + hp * table_stride(g) + kPad : nullptr;
   float* const my_sums = BIAS ? sums + wave * by_distance_floats(g) : nullptr;
   float far_sum = 0.f;
   if (SPLIT && BIAS) __syncthreads();
 
-  constexpr int kTogether = SPLIT ? kWave : kThreads;
-  typedef Stream<T, DP, kTogether> Load;
-  const int part = SPLIT ? 0 : wave;  // of a tile's load
-  const uint32_t lds_at = lds_address(smem_raw);
-  constexpr uint32_t kTileBytes = kTileElems * sizeof(T);
   floatx16_t acc[DP / 32];
   uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
   // A tile goes by in three passes of matrix instructions, with the arithmetic between them: d_out V^T, and the probabilities;
@@ -325,15 +342,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) acc[b] = floatx16_t{};
     if constexpr (SPLIT) {
-      T* const kt = lds + wave * 2 * kTileElems;
-      const uint32_t k_at = lds_at + wave * 2 * kTileBytes;
-      Load k_tiles(k, g.k_stride, 32 * wave, w.len, g.d, 0, 0, lane), v_tiles(v, g.v_stride, 32 * wave, w.len, g.d, 0, 0, lane);
-      const auto load = [&] {
-        k_tiles.load(k_at, 0, kWaves);
-        v_tiles.load(k_at + kTileBytes, 0, kWaves);
-      };
-      const int tiles = last_tok / 32 + 1;
-      if (wave < tiles) load();
+      T* const kt = lds + k_slot(0);
       for (int t = wave; t < tiles; t += kWaves) {
         landed<0>();
         if (clean) Load::clean(kt, 0, lane);
@@ -343,7 +352,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
         if (one_tile && !clean) own_delta(kt + kTileElems, s);
         attend(kt, kt + kTileElems, kt, s, s, 32 * t, clean, no);
         lds_done();
-        if (t + kWaves < tiles) load();
+        load(t + kWaves, t + kWaves);
       }
       if (!clean) write_delta();
       __syncthreads();
@@ -354,18 +363,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
       __syncthreads();
       join_parts<DP>(parts, kPart, wave, lane, joined);
     } else {
-      const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);
-      const int tiles = (end_tok + 31) / 32;
-      constexpr int kKs = S::kFew ? 3 : 4, kVs = S::kFew ? 2 : 4;
-      const auto k_slot = [&](int t) { return t % kKs * kTileElems; };
-      const auto v_slot = [&](int t) { return (kKs + t % kVs) * kTileElems; };
       const auto k_tile = [&](int t) { return lds + k_slot(t); };
       const auto v_tile = [&](int t) { return lds + v_slot(t); };
-      Load k_tiles(k, g.k_stride, 0, w.len, g.d, 0, part, lane), v_tiles(v, g.v_stride, 0, w.len, g.d, 0, part, lane);
-      const auto load = [&](int kt, int vt) {  // (each in turn)
-        if (kt < tiles) k_tiles.load(lds_at + k_slot(kt) * sizeof(T), part);
-        if (vt < tiles) v_tiles.load(lds_at + v_slot(vt) * sizeof(T), part);
-      };
       // K up to tile t and V up to the one before are there, for all wavefronts, and the tiles before t - 1 have been read:
       // their place takes others.
       const auto arrive = [&](int t) {
@@ -376,8 +375,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
         if (S::kFew) load(t + 1, t == 0 ? tiles : t);  // (the first V has been asked for)
         else load(t + 2, t + 2);
       };
-      load(0, 0);
-      if (!S::kFew) load(1, 1);
       arrive(0);
       floatx16_t s, next;
       form_scores(k_tile(0), s);
@@ -409,6 +406,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DP == 64 ? 2 : 1) void 
     check = sum_of_halves(check);
     spoilt = there && check != 0.f;
     if (!__syncthreads_or(spoilt)) break;
+    k_tiles.start(k, g.k_stride, 32 * first_tile, w.len, g.d, 0);
+    v_tiles.start(v, g.v_stride, 32 * first_tile, w.len, g.d, 0);
+    load_first();
   }
   if (there) {
     T* const mine = dq + tok * g.dq_stride + hp * g.d;
@@ -496,7 +496,7 @@ __device__ void sum_key(const PackedAttn& g, const SeqTile& w, int kv, int key, 
 }
 
 template <typename T, int DP, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_kernel(PackedAttn g) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void attn_packed_keys_kernel(PackedAttn g) {
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
   typedef Keys<T, DP, SPLIT> S;
@@ -726,9 +726,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
       T* const mine = lds + wave * 2 * kTileElems;
       float* const stat = stats + wave * S::kStat;
       const uint32_t tile_at = lds_at + wave * 2 * kTileBytes, stat_at = stats_at + wave * kStatBytes;
-      const auto of_heads = [&](int sub) {
-        begin(stream, sub, wave);
-        if (wave < tiles) load(stream, tile_at, stat_at);
+      const auto of_heads = [&] {
         for (int t = wave; t < tiles; t += kWaves) {
           landed<0>();
           if (clean) {
@@ -745,12 +743,14 @@ __global__ __launch_bounds__(kThreads, DP == 64 ? 2 : 1) void attn_packed_keys_k
         }
       };
       for (int sub = 0; sub < subs; ++sub) {
+        begin(stream, sub, wave);
+        if (wave < tiles) load(stream, tile_at, stat_at);
         if (BIAS) {
           __syncthreads();  // (the heads before are done with their bias)
           fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
           __syncthreads();
         }
-        of_heads(sub);
+        of_heads();
       }
       float* const parts = reinterpret_cast<float*>(smem_raw);
       constexpr size_t kPart = 2 * kTileElems * sizeof(T) / sizeof(float);

@@ -60,7 +60,6 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
   SeqTile w;
   const int slot = static_cast<int>(blockIdx.x) / subs;
   if (!(SPLIT ? find_tile</*LAST_FIRST=*/true>(g, slot, kRowsLog, g.pack, &w) : find_ranked_tile(g, slot, kRowsLog, g.pack, &w))) return;
-  if (BIAS) fill_bias<T, kThreads>(g, head0, bias);
 
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -84,14 +83,32 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
                                    left > 0 ? static_cast<uint32_t>((left - 1) * g.q_stride + heads * g.d) * static_cast<uint32_t>(sizeof(T)) : 0u);
     load_row_frags<T, DP>(b, (static_cast<uint32_t>(tok - first_tok) * static_cast<uint32_t>(g.q_stride) + hp * g.d) * static_cast<uint32_t>(sizeof(T)), g.d, lane, qf);
   }
-  const float* const my_bias = BIAS ? bias + hp * table_stride(g) + kPad : nullptr;
-  if (SPLIT && BIAS) __syncthreads();
-
   constexpr int kTogether = SPLIT ? kWave : kThreads;
   typedef Stream<T, DP, kTogether> Load;
   const int part = SPLIT ? 0 : wave;  // of a tile's load
   const uint32_t lds_at = lds_address(smem_raw);
   constexpr uint32_t kTileBytes = kTileElems * sizeof(T);
+  // SPLIT: the wavefronts deal the tiles up to the last one that the rows see; else the workgroup's rows see these
+  const int end_tok = SPLIT ? last_tok + 1 : min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);
+  const int tiles = (end_tok + 31) / 32;  // (a wavefront's last ones may be all masked: leaving them out would save nothing)
+  const int first_tile = SPLIT ? wave : 0, every = SPLIT ? kWaves : 1;
+  Load k_tiles(k, g.k_stride, 32 * first_tile, w.len, g.d, 0, part, lane), v_tiles(v, g.v_stride, 32 * first_tile, w.len, g.d, 0, part, lane);
+  const auto slot_of = [&](int t) { return (SPLIT ? wave : t % S::kCopies) * 2 * kTileElems; };
+  const auto load_k = [&](int t) { k_tiles.load(lds_at + slot_of(t) * sizeof(T), part, every); };
+  const auto load_v = [&](int t) { v_tiles.load(lds_at + slot_of(t) * sizeof(T) + kTileBytes, part, every); };
+  const auto load_first = [&] {
+#pragma unroll
+    for (int t = 0; t < (SPLIT || S::kCopies < 4 ? 1 : 2); ++t)
+      if (first_tile + t < tiles) {
+        load_k(t);
+        load_v(t);
+      }
+  };
+  load_first();  // (ahead of what the bias waits for)
+  const float* const my_bias = BIAS ? bias + hp * table_stride(g) + kPad : nullptr;
+  if (BIAS) fill_bias<T, kThreads>(g, head0, bias);
+  if (SPLIT && BIAS) __syncthreads();
+
   floatx16_t o[DP / 32];
   float m, total;
   uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
@@ -218,15 +235,8 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
     total = 0.f;     // this half's share of the sum
     if constexpr (SPLIT) {
       // one tile of each: K's next one is requested when the scores are there, V's at the end
-      T* const kt = lds + wave * 2 * kTileElems;
-      T* const vt = kt + kTileElems;
-      const uint32_t k_at = lds_at + wave * 2 * kTileBytes, v_at = k_at + kTileBytes;
-      Load k_tiles(k, g.k_stride, 32 * wave, w.len, g.d, 0, 0, lane), v_tiles(v, g.v_stride, 32 * wave, w.len, g.d, 0, 0, lane);
-      const int tiles = last_tok / 32 + 1;
-      if (wave < tiles) {
-        k_tiles.load(k_at, 0, kWaves);
-        v_tiles.load(v_at, 0, kWaves);
-      }
+      const T* const kt = lds + slot_of(0);
+      T* const vt = lds + slot_of(0) + kTileElems;
       for (int t = wave; t < tiles; t += kWaves) {
         const bool more = t + kWaves < tiles;
         landed<Load::kLoads>();
@@ -234,7 +244,7 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
         form_scores(kt, vt, s);
         lds_done();
         if (more) {
-          k_tiles.load(k_at, 0, kWaves);
+          load_k(t);
           landed<Load::kLoads>();
         } else {
           landed<0>();
@@ -244,27 +254,20 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
         float top = largest(s);
         attend(kt, vt, s, s, 0, top, no);
         lds_done();
-        if (more) v_tiles.load(v_at, 0, kWaves);
+        if (more) load_v(t);
       }
     } else {
-      const int end_tok = min(((w.tile + 1) << kRowsLog) >> g.pack, w.len);  // of the workgroup: the keys it sees
-      const int tiles = (end_tok + 31) / 32;  // (a wavefront's last ones may be all masked: leaving them out would save nothing)
-      Load k_tiles(k, g.k_stride, 0, w.len, g.d, 0, part, lane), v_tiles(v, g.v_stride, 0, w.len, g.d, 0, part, lane);
-      const auto slot = [&](int t) { return t % S::kCopies * 2 * kTileElems; };
-      const auto load = [&](int t) {
-        k_tiles.load(lds_at + slot(t) * sizeof(T), part);
-        v_tiles.load(lds_at + slot(t) * sizeof(T) + kTileBytes, part);
-      };
       // Tiles up to t are there, for all wavefronts, and those before t - 1 have been read: their place takes another.
       const auto arrive = [&](int t) {
         if (S::kCopies == 4 && t + 1 < tiles) landed<2 * Load::kLoads>();
         else landed<0>();
-        if (clean) Load::clean(lds + slot(t) + kTileElems, part, lane);
+        if (clean) Load::clean(lds + slot_of(t) + kTileElems, part, lane);
         __syncthreads();
-        if (t + S::kCopies - 2 < tiles) load(t + S::kCopies - 2);
+        if (t + S::kCopies - 2 < tiles) {
+          load_k(t + S::kCopies - 2);
+          load_v(t + S::kCopies - 2);
+        }
       };
-      load(0);
-      if (S::kCopies == 4 && tiles > 1) load(1);
       arrive(0);
       floatx16_t s, next;
       form_scores(lds, lds, s);
@@ -273,10 +276,10 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
       int t = 0;
       for (; t + 1 < tiles; ++t) {
         arrive(t + 1);
-        attend(lds + slot(t + 1), lds + slot(t) + kTileElems, s, next, 32 * (t + 1), top, yes);
+        attend(lds + slot_of(t + 1), lds + slot_of(t) + kTileElems, s, next, 32 * (t + 1), top, yes);
         s = next;
       }
-      attend(lds + slot(t), lds + slot(t) + kTileElems, s, s, 0, top, no);
+      attend(lds + slot_of(t), lds + slot_of(t) + kTileElems, s, s, 0, top, no);
     }
     total = sum_of_halves(total);
     if constexpr (SPLIT) {
@@ -316,6 +319,9 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
     check = sum_of_halves(check);
     spoilt = there && check != 0.f;
     if (!__syncthreads_or(spoilt)) break;
+    k_tiles.start(k, g.k_stride, 32 * first_tile, w.len, g.d, 0);
+    v_tiles.start(v, g.v_stride, 32 * first_tile, w.len, g.d, 0);
+    load_first();
   }
   const float inverse = total == 0.f ? 0.f : 1.f / total;
   T* const mine = out + tok * g.out_stride + hp * g.d;
