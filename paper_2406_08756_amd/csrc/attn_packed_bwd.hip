@@ -714,6 +714,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
       in_order();
     }
   };
+  // (waited for here, or the compiler waits in every turn of the loop that uses them first, for the tiles on their way too)
+  const auto have_values = [&] {
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i) stay(vf[i]);
+  };
   constexpr std::true_type yes;
   constexpr std::false_type no;
 
@@ -727,6 +732,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
       float* const stat = stats + wave * S::kStat;
       const uint32_t tile_at = lds_at + wave * 2 * kTileBytes, stat_at = stats_at + wave * kStatBytes;
       const auto of_heads = [&] {
+        have_values();
         for (int t = wave; t < tiles; t += kWaves) {
           landed<0>();
           if (clean) {
@@ -792,6 +798,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
       load_next(0);
       if (S::kCopies == 4 && steps > 1) load_next(1);
       arrive(0);
+      have_values();
       floatx16_t s, next, offset;
       form_scores(tile(0), s);
       offsets(stat(0), first_row, offset);

@@ -237,6 +237,9 @@ __global__ __launch_bounds__(kThreads, SPLIT && sizeof(T) * DP == 512 ? 1 : 2) v
       // one tile of each: K's next one is requested when the scores are there, V's at the end
       const T* const kt = lds + slot_of(0);
       T* const vt = lds + slot_of(0) + kTileElems;
+      // (waited for here, or the compiler waits in every turn of the loop, for the tiles on their way too)
+#pragma unroll
+      for (int i = 0; i < L::kSteps; ++i) stay(qf[i]);
       for (int t = wave; t < tiles; t += kWaves) {
         const bool more = t + kWaves < tiles;
         landed<Load::kLoads>();
