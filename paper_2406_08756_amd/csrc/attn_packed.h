@@ -42,6 +42,8 @@ __device__ __forceinline__ float max_of_halves(float v) {
 __device__ __forceinline__ void forget(uint32_t& x) { asm volatile("" : "+v"(x)); }
 // x is computed before this point, not where it is used.
 template <typename X> __device__ __forceinline__ void stay(X& x) { asm volatile("" : "+v"(x)); }
+// Likewise sums of matrix instructions, in the accumulation registers: they are not copied from there before this point.
+__device__ __forceinline__ void stay_summed(floatx16_t& x) { asm volatile("" : "+a"(x)); }
 // What stands above is issued before anything below.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

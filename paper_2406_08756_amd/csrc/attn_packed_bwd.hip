@@ -495,6 +495,26 @@ __device__ void sum_key(const PackedAttn& g, const SeqTile& w, int kv, int key, 
     }
 }
 
+// d_table[b, h] = the sum over row tiles of their shares, for one head, in one order: interleaved sums, then those in turn.
+template <typename T>
+__device__ void sum_table(const PackedAttn& g, int h, float* sums, T* d_table) {
+  int width = 1;
+  while (width < g.buckets) width *= 2;
+  const int b = static_cast<int>(threadIdx.x) & (width - 1), y = static_cast<int>(threadIdx.x) / width, together = kThreads / width;
+  const float* const at = g.partials + static_cast<long long>(h) * g.buckets + b;
+  const long long step = static_cast<long long>(g.heads) * g.buckets;
+  float sum = 0.f;
+  if (b < g.buckets) {
+#pragma unroll 8
+    for (int s = y; s < g.row_slots; s += together) sum += at[s * step];
+  }
+  sums[threadIdx.x] = sum;
+  __syncthreads();
+  if (y != 0 || b >= g.buckets) return;
+  for (int i = 1; i < together; ++i) sum += sums[i * width + b];
+  store1(d_table + static_cast<long long>(b) * g.heads + h, sum);
+}
+
 template <typename T, int DP, bool BIAS, bool SPLIT>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void attn_packed_keys_kernel(PackedAttn g) {
   typedef Tile<T, DP> L;
@@ -507,6 +527,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
   float* const bias = reinterpret_cast<float*>(smem_raw + S::kLds);
 
   const int kv = static_cast<int>(blockIdx.x) % g.kv_heads, slot = static_cast<int>(blockIdx.x) / g.kv_heads;
+  if (BIAS && slot >= g.key_slots) {
+    sum_table(g, static_cast<int>(blockIdx.x) - g.key_slots * g.kv_heads, reinterpret_cast<float*>(smem_raw), static_cast<T*>(g.d_table));
+    return;
+  }
   SeqTile w;
   if (SPLIT || g.sequences > kRankedSequences) {
     if (!find_tile</*LAST_FIRST=*/false>(g, slot, kKeysLog, 0, &w)) return;
@@ -580,7 +604,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
     r.row += every * 32;
     r.left -= every;
   };
-  constexpr int kMostLoads = 2 * Load::kLoads + 2;  // (of the wavefront that has the statistics; the others have two less)
 
   floatx16_t dk[DP / 32], dv[DP / 32];
   uint32_t row_base = L::row_base(lane), col_base = L::col_base(lane);
@@ -643,14 +666,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
       for (int i = 0; i < 16; ++i) offset[i] += x[i];
     }
   };
-  // s: the scores of the tile from row r0 on, `offset` their offsets; leaves those of the next one in `next` and `offset`.
+  // s: the scores of the tile from row r0 on, `offset` their offsets; leaves those of the next one in `next` and `offset`, and
+  // its first fragments (as first_frags() does) in the ring.  between() comes in the third pass.  What a pass leaves is used
+  // some steps into the next, whose matrix instructions do not need it: by then it is there.
   const auto attend = [&](const T* tile, const float* stat, int r0, const T* next_tile, const float* next_stat, int next_r0, floatx16_t& s,
-                          floatx16_t& next, floatx16_t& offset, auto has_next) {
+                          floatx16_t& next, floatx16_t& offset, auto has_next, auto between) {
     constexpr bool NEXT = decltype(has_next)::value;
-    first_frags(tile, next_tile, 0);
+    constexpr int kGroup = 16 / L::kGroups, kLag = L::kSteps >= 8 ? 2 : 1;
+    constexpr bool kSummed = sizeof(T) * DP > 128;  // (a wavefront has more than 256 registers)
+    forget(row_base);
+    forget(col_base);
     const auto turn = [&](int i) {  // the i-th of the fragments that are used has been: without a next tile its own are left out
       const int n = NEXT || i + kRing < L::kSteps ? i + kRing : i + kRing + L::kSteps;
       if (n < kFrags) ring[i % kRing] = frag(tile, next_tile, n);
+      else if (NEXT) ring[i % kRing] = frag(next_tile, next_tile, n - kFrags);
     };
     floatx16_t dp{}, delta, next_bias;  // (read ahead of their use, as the fragments are)
     per_row(stat + kWave, delta);
@@ -681,11 +710,24 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
         Op::mma(next, ring[i % kRing], kf[i]);
         turn(L::kSteps + i);
       }
+      if (kSummed && NEXT && i == kLag) stay_summed(dp);
+      if (i < kLag) {
 #pragma unroll
-      for (int e = i * 16 / L::kSteps; e < (i + 1) * 16 / L::kSteps; ++e) {
-        float x = s[e] * (dp[e] - delta[e]);
-        if (NEXT) stay(x);
-        dp[e] = x;
+        for (int c = i * L::kGroups / kLag; c < (i + 1) * L::kGroups / kLag; ++c) {
+          p[c] = Op::from_acc(s, c);
+          if (NEXT) stay(p[c]);
+        }
+      } else {
+#pragma unroll
+        for (int e = (i - kLag) * 16 / (L::kSteps - kLag); e < (i + 1 - kLag) * 16 / (L::kSteps - kLag); ++e) {
+          float x = s[e] * (dp[e] - delta[e]);
+          if (NEXT) stay(x);
+          dp[e] = x;
+          if (e % kGroup == kGroup - 1) {
+            ds[e / kGroup] = Op::from_acc(dp, e / kGroup);
+            if (NEXT) stay(ds[e / kGroup]);
+          }
+        }
       }
       if (NEXT && BIAS) read_bias(next_r0, i * 16 / L::kSteps, (i + 1) * 16 / L::kSteps, next_bias);
       if (NEXT) in_order();
@@ -694,11 +736,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (apart + (acc_row(e, 0) >> g.pack) < 0) dp[e] = 0.f;
-    }
 #pragma unroll
-    for (int c = 0; c < L::kGroups; ++c) {
-      p[c] = Op::from_acc(s, c);
-      ds[c] = Op::from_acc(dp, c);
+      for (int c = 0; c < L::kGroups; ++c) ds[c] = Op::from_acc(dp, c);
     }
     if (NEXT) per_row(next_stat, offset);
 #pragma unroll
@@ -712,8 +751,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
         for (int n = i * 16 / kCols; n < (i + 1) * 16 / kCols; ++n) offset[n] += next_bias[n];
       }
       in_order();
+      if (i == kCols / 4) between();
     }
   };
+  const auto nothing = [] {};
   // (waited for here, or the compiler waits in every turn of the loop that uses them first, for the tiles on their way too)
   const auto have_values = [&] {
 #pragma unroll
@@ -743,7 +784,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
           floatx16_t s, offset;
           form_scores(mine, s);
           offsets(stat, r0, offset);
-          attend(mine, stat, r0, mine, stat, r0, s, s, offset, no);
+          first_frags(mine, mine, 0);
+          attend(mine, stat, r0, mine, stat, r0, s, s, offset, no, nothing);
           lds_done();
           if (t + kWaves < tiles) load(stream, tile_at, stat_at);
         }
@@ -774,47 +816,56 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
       const auto tile = [&](int it) { return lds + slot(it) * 2 * kTileElems; };
       const auto stat = [&](int it) { return stats + slot(it) * S::kStat; };
       const auto load_next = [&](int it) { load(stream, lds_at + slot(it) * 2 * kTileBytes, stats_at + slot(it) * kStatBytes); };
-      int ahead = 0, sub = 0;  // tile `it + 1`: its number among those of its heads, and which heads
-      // Tiles up to `it` are there, for all wavefronts, and those before it - 1 have been read: their place takes another.
+      // With four places two tiles are in use, another there or on its way, and the last one's place takes the one after: asked
+      // for a tile's time before the wait for it, in the third pass of the tile two before it.  With three it is the tile before.
+      constexpr bool kBetween = S::kCopies == 4;
+      // Tile `it` is there, for all wavefronts, and those before it - 2 (it - 1) have been read.
+      const auto clean_tile = [&](int it) {
+        Load::clean(tile(it), part, lane);
+        Load::clean(tile(it) + kTileElems, part, lane);
+      };
       const auto arrive = [&](int it) {
-        if (S::kCopies == 4 && it + 1 < steps) {
-          if (part == 0) landed<kMostLoads>();
-          else landed<kMostLoads - 2>();
-        } else {
-          landed<0>();
-        }
-        if (clean) {
-          Load::clean(tile(it), part, lane);
-          Load::clean(tile(it) + kTileElems, part, lane);
-        }
-        if (BIAS && ahead == 0) {
-          __syncthreads();  // (the offsets of the heads before are done)
-          fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
-        }
+        landed<0>();
+        if (clean) clean_tile(it);
         __syncthreads();
-        if (it + S::kCopies - 2 < steps) load_next(it + S::kCopies - 2);
+        if (it + 1 < steps) load_next(it + 1);
+      };
+      const auto heads_bias = [&](int sub) {
+        __syncthreads();  // (the offsets of the heads before are done)
+        fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
+        __syncthreads();
       };
       begin(stream, 0, 0);
       load_next(0);
-      if (S::kCopies == 4 && steps > 1) load_next(1);
-      arrive(0);
+      const int first = kBetween && steps > 1 ? 1 : 0;
+      if (first == 1) {
+        load_next(1);
+        landed<0>();
+        if (clean) clean_tile(0);
+      }
+      arrive(first);
+      if (BIAS) heads_bias(0);
       have_values();
       floatx16_t s, next, offset;
       form_scores(tile(0), s);
       offsets(stat(0), first_row, offset);
-      int it = 0, r0 = first_row;
+      first_frags(tile(0), tile(0), 0);
+      int it = 0, r0 = first_row, ahead = 0, sub = 0;  // ahead: tile it + 1's number among those of its heads, which `sub` are
       for (; it + 1 < steps; ++it) {
         if (++ahead == tiles) {
           ahead = 0;
           ++sub;
+          if (BIAS) heads_bias(sub);
         }
         const int next_r0 = first_row + 32 * ahead;
-        arrive(it + 1);
-        attend(tile(it), stat(it), r0, tile(it + 1), stat(it + 1), next_r0, s, next, offset, yes);
+        if (!kBetween) arrive(it + 1);
+        attend(tile(it), stat(it), r0, tile(it + 1), stat(it + 1), next_r0, s, next, offset, yes, [&] {
+          if (kBetween && it + 2 < steps) arrive(it + 2);
+        });
         s = next;
         r0 = next_r0;
       }
-      attend(tile(it), stat(it), r0, tile(it), stat(it), r0, s, s, offset, no);
+      attend(tile(it), stat(it), r0, tile(it), stat(it), r0, s, s, offset, no, nothing);
     }
     if (clean) break;
     float check = 0.f;
@@ -857,37 +908,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
   }
 }
 
-// d_table[b, h] = the sum over row tiles of their shares, in one order: 16 interleaved sums, then those in turn.
-constexpr int kTableWaves = 16;
-template <typename T>
-__global__ __launch_bounds__(kTableWaves * kWave) void attn_packed_table_kernel(const float* partials, T* d_table, int slots, int heads, int buckets) {
-  __shared__ float sums[kTableWaves][kWave];
-  const int h = blockIdx.x, b = threadIdx.x & (kWave - 1), y = threadIdx.x / kWave;
-  float sum = 0.f;
-  if (b < buckets)
-    for (int s = y; s < slots; s += kTableWaves) sum += partials[(static_cast<long long>(s) * heads + h) * buckets + b];
-  sums[y][b] = sum;
-  __syncthreads();
-  if (y != 0 || b >= buckets) return;
-  for (int i = 1; i < kTableWaves; ++i) sum += sums[i][b];
-  store1(d_table + static_cast<long long>(b) * heads + h, sum);
-}
-
 template <typename T, int DP, bool BIAS>
 hipError_t launch_bwd(const PackedAttn& g, hipStream_t st) {
   const size_t table = BIAS ? static_cast<size_t>(table_floats(g)) * sizeof(float) : 0;
   const size_t by_row = table + (BIAS ? kWaves * by_distance_floats(g) * sizeof(float) : 0);
-  const size_t slots = attn_packed_row_slots(g, g.split_rows), key_groups = attn_packed_key_slots(g) * g.kv_heads;
-  const size_t row_groups = slots * (g.heads >> g.pack);
+  const size_t row_groups = static_cast<size_t>(g.row_slots) * (g.heads >> g.pack), key_groups = static_cast<size_t>(g.key_slots) * g.kv_heads;
   hipError_t e = g.split_rows ? launch_packed<attn_packed_rows_kernel<T, DP, BIAS, true>>(row_groups, Rows<T, DP, BIAS, true>::kLds + by_row, g, st)
                               : launch_packed<attn_packed_rows_kernel<T, DP, BIAS, false>>(row_groups, Rows<T, DP, BIAS, false>::kLds + by_row, g, st);
   if (e != hipSuccess) return e;
-  e = g.split_keys ? launch_packed<attn_packed_keys_kernel<T, DP, BIAS, true>>(key_groups, Keys<T, DP, true>::kLds + table, g, st)
-                   : launch_packed<attn_packed_keys_kernel<T, DP, BIAS, false>>(key_groups, Keys<T, DP, false>::kLds + table, g, st);
-  if (e != hipSuccess || !BIAS) return e;
-  hipLaunchKernelGGL((attn_packed_table_kernel<T>), dim3(g.heads), dim3(kTableWaves * kWave), 0, st, g.partials, static_cast<T*>(g.d_table),
-                     static_cast<int>(slots), g.heads, g.buckets);
-  return hipGetLastError();
+  // (behind the key tiles a workgroup per head joins the table's gradient: a launch of its own was 4 us)
+  const size_t groups = key_groups + (BIAS ? g.heads : 0);
+  return g.split_keys ? launch_packed<attn_packed_keys_kernel<T, DP, BIAS, true>>(groups, Keys<T, DP, true>::kLds + table, g, st)
+                      : launch_packed<attn_packed_keys_kernel<T, DP, BIAS, false>>(groups, Keys<T, DP, false>::kLds + table, g, st);
 }
 template <typename T, int DP>
 hipError_t launch_bwd(const PackedAttn& g, hipStream_t st) {

@@ -395,10 +395,12 @@ void attn_packed_choose(int dtype, PackedAttn* g) {
   g->split_rows = g->split_fwd && attn_packed_split_rows_fit(dtype, *g);
   g->split_keys = 0;
   g->split_keys = attn_packed_key_slots(*g) * g->kv_heads < 2 * key_groups(g->d) || g->tokens / g->sequences < kShort;
+  g->row_slots = static_cast<int>(attn_packed_row_slots(*g, g->split_rows));
+  g->key_slots = static_cast<int>(attn_packed_key_slots(*g));
 }
 bool attn_packed_fits(const PackedAttn& g) {
   const long long subs = g.heads >> g.pack, fwd = static_cast<long long>(attn_packed_row_slots(g, g.split_fwd)) * subs;
-  const long long rows = static_cast<long long>(attn_packed_row_slots(g, g.split_rows)) * subs, keys = static_cast<long long>(attn_packed_key_slots(g)) * g.kv_heads;
+  const long long rows = static_cast<long long>(attn_packed_row_slots(g, g.split_rows)) * subs, keys = static_cast<long long>(attn_packed_key_slots(g)) * g.kv_heads + g.heads;
   return fits_grid(fwd, kThreads) && fits_grid(rows, kThreads) && fits_grid(keys, kThreads);
 }
 size_t attn_packed_row_slots(const PackedAttn& g, bool split) {
