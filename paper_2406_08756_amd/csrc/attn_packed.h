@@ -399,7 +399,7 @@ __device__ __forceinline__ void store4(float* p, float a, float b, float c, floa
 // Bias by distance, times log2 e: `far` distances, and kPad more on both sides so that the reads of a 32-row strip against
 // 64 keys that holds one near or masked pair need no limits.
 constexpr int kPad = 96;
-__host__ __device__ __forceinline__ int table_stride(const PackedAttn& g) { return g.far + 2 * kPad; }
+__host__ __device__ __forceinline__ int table_stride(const PackedAttn& g) { return (g.far + 2 * kPad + 3) & ~3; }  // (what follows is read 16 bytes at a time)
 __host__ __device__ __forceinline__ int table_floats(const PackedAttn& g) { return table_stride(g) << g.pack; }
 __device__ __forceinline__ int bucket_of(const PackedAttn& g, int distance) {
   // (all kMaxBuckets starts, those behind the last bucket at the largest number: a loop to the last would wait for each)

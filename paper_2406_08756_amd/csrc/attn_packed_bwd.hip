@@ -16,7 +16,7 @@ namespace {
 // (47 diagonals; which places of a diagonal exist depends on the row alone, the others stay zero), and a lane adds up one of
 // them, so that each sum has one owner and one order.  Blocks whose keys are all far are summed in a register.
 constexpr int kDiagonalStride = 20, kBlockFloats = 47 * kDiagonalStride + 20;
-__host__ __device__ __forceinline__ int distances(const PackedAttn& g) { return g.far + 64; }
+__host__ __device__ __forceinline__ int distances(const PackedAttn& g) { return (g.far + 64 + 3) & ~3; }
 __host__ __device__ __forceinline__ int by_distance_floats(const PackedAttn& g) { return (distances(g) << g.pack) + kBlockFloats; }  // of a wavefront
 
 // K and V in tiles of 32 keys: four of each, which leaves a tile the time of two to arrive, or three and two where the sums of
@@ -69,7 +69,7 @@ __device__ void sum_row_dq(const PackedAttn& g, const T* q, const T* d_out, cons
 }
 
 template <typename T, int DP, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 || (DP == 64 && !SPLIT) ? 2 : 1) void attn_packed_rows_kernel(PackedAttn g) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 4 && (SPLIT || DP == 128)) || (SPLIT && BIAS && DP == 128) ? 1 : 2) void attn_packed_rows_kernel(PackedAttn g) {
   typedef Tile<T, DP> L;
   typedef Operand<T> Op;
   typedef Rows<T, DP, BIAS, SPLIT> S;
@@ -125,6 +125,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || (DP == 64 && !SPLIT) ? 
     load(first_tile, first_tile);
     if (!SPLIT && !S::kFew) load(1, 1);
   };
+  load_first();
 
   typename Op::Frag qf[L::kSteps], gf[L::kSteps];  // Q and d_out
   float delta = 0.f, lse2 = kInf;
@@ -136,17 +137,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 || (DP == 64 && !SPLIT) ? 
     const auto at = [&](long long stride) {
       return (static_cast<uint32_t>(tok - first_tok) * static_cast<uint32_t>(stride) + hp * g.d) * static_cast<uint32_t>(sizeof(T));
     };
-    // all loads on their way before the first is waited for, the first tiles' and the bias's too
+    // (all loads on their way before the first is waited for)
     typename Op::Frag of[L::kSteps];
     load_row_frags<T, DP>(buffer(out, g.out_stride), at(g.out_stride), g.d, lane, of);
     load_row_frags<T, DP>(buffer(d_out, g.out_stride), at(g.out_stride), g.d, lane, gf);
     load_row_frags<T, DP>(buffer(q, g.q_stride), at(g.q_stride), g.d, lane, qf);
     float lse = -kInf;
     if (there) lse = g.lse[static_cast<long long>(head0 + hp) * g.tokens + w.start + tok];
-    load_first();
     if (BIAS) {
       fill_bias<T, kThreads>(g, head0, bias);
-      for (int x = threadIdx.x; x < kWaves * by_distance_floats(g); x += kThreads) sums[x] = 0.f;
+      for (int x = 4 * threadIdx.x; x < kWaves * by_distance_floats(g); x += 4 * kThreads) *reinterpret_cast<float4*>(sums + x) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
     for (int s = 0; s < L::kSteps; ++s) delta += Op::dot(of[s], gf[s]);
