@@ -29,7 +29,9 @@ template <typename T, int DP, bool BIAS, bool SPLIT> struct Rows {
   static constexpr size_t kLds = kTiles + (SPLIT ? kWaves * sizeof(uint32_t) : 0);
 };
 template <typename T, int DP, bool SPLIT> struct Keys {
-  static constexpr int kTileElems = 32 * DP, kCopies = SPLIT ? kWaves : sizeof(T) * DP == 512 ? 3 : 4;
+  // of a wavefront (SPLIT): the tile at work and the next one on its way, where there is room
+  static constexpr int kPlaces = sizeof(T) * DP == 512 ? 1 : 2;
+  static constexpr int kTileElems = 32 * DP, kCopies = SPLIT ? kPlaces * kWaves : sizeof(T) * DP == 512 ? 3 : 4;
   static constexpr size_t kTiles = 2 * kCopies * static_cast<size_t>(kTileElems) * sizeof(T);
   static constexpr int kStat = 2 * kWave;  // floats of a tile's statistics: offset, delta, each as a wavefront loads them
   static constexpr size_t kLds = kTiles + kCopies * kStat * sizeof(float) + (SPLIT ? kWaves * sizeof(uint32_t) : 0);
@@ -769,13 +771,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = floatx16_t{};
     if constexpr (SPLIT) {
-      T* const mine = lds + wave * 2 * kTileElems;
-      float* const stat = stats + wave * S::kStat;
-      const uint32_t tile_at = lds_at + wave * 2 * kTileBytes, stat_at = stats_at + wave * kStatBytes;
+      const auto place = [&](int n) { return wave * S::kPlaces + n % S::kPlaces; };
+      const auto load_next = [&](int n) { load(stream, lds_at + place(n) * 2 * kTileBytes, stats_at + place(n) * kStatBytes); };
       const auto of_heads = [&] {
         have_values();
-        for (int t = wave; t < tiles; t += kWaves) {
-          landed<0>();
+        for (int t = wave, n = 0; t < tiles; t += kWaves, ++n) {
+          T* const mine = lds + place(n) * 2 * kTileElems;
+          const float* const stat = stats + place(n) * S::kStat;
+          if (S::kPlaces == 2 && t + kWaves < tiles) {
+            load_next(n + 1);
+            landed<2 * Load::kLoads + 2>();
+          } else {
+            landed<0>();
+          }
           if (clean) {
             Load::clean(mine, 0, lane);
             Load::clean(mine + kTileElems, 0, lane);
@@ -787,12 +795,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
           first_frags(mine, mine, 0);
           attend(mine, stat, r0, mine, stat, r0, s, s, offset, no, nothing);
           lds_done();
-          if (t + kWaves < tiles) load(stream, tile_at, stat_at);
+          if (S::kPlaces == 1 && t + kWaves < tiles) load_next(n + 1);
         }
       };
       for (int sub = 0; sub < subs; ++sub) {
         begin(stream, sub, wave);
-        if (wave < tiles) load(stream, tile_at, stat_at);
+        if (wave < tiles) load_next(0);
         if (BIAS) {
           __syncthreads();  // (the heads before are done with their bias)
           fill_bias<T, kThreads>(g, kv * group + (sub << g.pack), bias);
@@ -900,7 +908,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
       }
   }
   uint32_t spoilt_keys = static_cast<uint32_t>(__ballot(spoilt));
-  if constexpr (SPLIT) spoilt_keys = share_rows(spoilt_keys, reinterpret_cast<uint32_t*>(stats + kWaves * S::kStat), wave);
+  if constexpr (SPLIT) spoilt_keys = share_rows(spoilt_keys, reinterpret_cast<uint32_t*>(stats + S::kCopies * S::kStat), wave);
   if (spoilt_keys != 0) __threadfence();
   for (uint32_t keys = spoilt_keys; keys != 0; keys &= keys - 1) {
     const int j = key0 + __builtin_ctz(keys);
