@@ -11,7 +11,7 @@
 // in which k is dealt to lanes and registers is free as long as A and B agree, and it is chosen so that the registers of D
 // are, rounded, the B operand of the next product, O^T += V^T P^T: no probability moves between lanes.
 #pragma once
-#include <mutex>
+#include <atomic>
 
 #include "kernels.h"
 #include "mfma_common.h"
@@ -421,10 +421,16 @@ __device__ __forceinline__ void fill_bias(const PackedAttn& g, int head0, float*
 constexpr int kMostLds = 159 << 10;  // (the barrier that joins a truth value has 1 KB of its own)
 template <auto KERNEL>
 hipError_t launch_packed(size_t groups, size_t lds, const PackedAttn& g, hipStream_t st) {
-  static std::once_flag once;
-  static hipError_t limit = hipSuccess;
-  std::call_once(once, [] { limit = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds); });
-  if (limit != hipSuccess) return limit;
+  static std::atomic<uint64_t> allowed{0};  // a bit per device (the first 64; for others every time)
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = device < 64 ? uint64_t{1} << device : 0;
+  if ((allowed.load(std::memory_order_relaxed) & bit) == 0) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds);
+    if (e != hipSuccess) return e;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
   hipLaunchKernelGGL(KERNEL, dim3(static_cast<unsigned>(groups)), dim3(kThreads), lds, st, g);
   return hipGetLastError();
 }
