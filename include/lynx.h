@@ -129,7 +129,8 @@ typedef struct {
 /* M_i of the paper's memory constraint (Eq. 8): bytes of activation act_id
  * (0..13) for this shape.  LayerNorm outputs (A1, A9) include their two fp32
  * per-token statistics, the context A6 two fp32 attention row statistics per
- * (batch element, head, row).  Returns 0 for a bad argument. */
+ * (batch element, head, row); A3 to A5 are 0 with LYNX_FLAG_PACKED_ATTENTION.
+ * Returns 0 for a bad argument. */
 size_t lynx_activation_bytes(const lynx_layer_config* cfg, int act_id);
 
 /* Workspace (device bytes) that lynx_layer_create needs so that
@@ -187,7 +188,7 @@ lynx_status lynx_layer_set_params(lynx_layer_t layer, const lynx_params* params)
 /* Layers with LYNX_FLAG_PACKED_ATTENTION only (else STATE; also STATE between forward and backward).
  * Sequence i of the next passes is tokens offsets[i] .. offsets[i+1] - 1; offsets (device, sequences + 1 entries) is
  * borrowed and read by the kernels of forward, regeneration and backward, so its values must not change in between.
- * A forward pass without sequences fails with STATE.  Errors: INVALID_ARG, STATE, SHAPE (sequences not in
+ * A pass without sequences (forward, recompute, backward; not a dry run) fails with STATE.  Errors: INVALID_ARG, STATE, SHAPE (sequences not in
  * 1 .. micro_batch + tokens / 16). */
 lynx_status lynx_layer_set_sequences(lynx_layer_t layer, const int32_t* offsets_device, int32_t sequences);
 /* The position bias of the next passes: bucket_starts (host, copied) as in lynx_attention_config, table_device and
@@ -403,7 +404,7 @@ lynx_status lynx_policy_layer_problem(const lynx_layer_config* cfg, lynx_policy_
  * (head h at column h head_dim of its token's row); the distance between tokens
  * is a stride of the config, so that q, k and v may be columns of one fused
  * projection, and d_q, d_k, d_v columns of its gradient.  bias_table and
- * d_bias_table [num_buckets, heads].  out shares its stride with d_out.  Gradients
+ * d_bias_table [num_buckets, heads].  out shares its stride with d_out.  Results
  * are overwritten and must not overlap any input or one another's elements.
  *
  * offsets (device, sequences + 1 entries, not decreasing, between 0 and tokens) is

@@ -1222,6 +1222,9 @@ lynx_status lynx_layer_set_params(lynx_layer_t L, const lynx_params* params) {
   return LYNX_OK;
 }
 
+// (a dry run may be switched off between its passes)
+static bool lacks_sequences(const lynx_layer_s* L) { return L->D.packed && L->offsets == nullptr && !L->dry; }
+
 lynx_status lynx_layer_set_sequences(lynx_layer_t L, const int32_t* offsets, int32_t sequences) {
   if (L == nullptr || offsets == nullptr || (reinterpret_cast<uintptr_t>(offsets) & 3u)) return LYNX_ERR_INVALID_ARG;
   if (!L->D.packed || L->book.state != 0) return LYNX_ERR_STATE;
@@ -1269,8 +1272,7 @@ lynx_status lynx_layer_forward(lynx_layer_t L, const void* x, void* out, uint32_
   if (L == nullptr || !aligned16(x) || !aligned16(out)) return LYNX_ERR_INVALID_ARG;
   if (retain_mask & ~0x3FFFu) return LYNX_ERR_INVALID_ARG;
   if (step >> 32) return LYNX_ERR_INVALID_ARG;
-  if (L->D.packed && L->offsets == nullptr && !L->dry) return LYNX_ERR_STATE;
-  if (!L->have_params || L->book.state != 0) return LYNX_ERR_STATE;
+  if (!L->have_params || L->book.state != 0 || lacks_sequences(L)) return LYNX_ERR_STATE;
   const void* old_x = L->x;
   void* old_out = L->out;
   const uint64_t old_step = L->step;
@@ -1284,7 +1286,7 @@ lynx_status lynx_layer_forward(lynx_layer_t L, const void* x, void* out, uint32_
 
 lynx_status lynx_recompute(lynx_layer_t L, uint32_t segment_mask, void* hip_stream) {
   if (L == nullptr) return LYNX_ERR_INVALID_ARG;
-  if (L->book.state != 1) return LYNX_ERR_STATE;
+  if (L->book.state != 1 || lacks_sequences(L)) return LYNX_ERR_STATE;
   return two_pass(L, static_cast<hipStream_t>(hip_stream),
                   [&](Ctx& cx) { return recompute_pass(cx, segment_mask); });
 }
@@ -1293,7 +1295,7 @@ lynx_status lynx_layer_backward(lynx_layer_t L, const void* d_out, void* d_x, co
                                 void* hip_stream) {
   if (L == nullptr || !aligned16(d_out) || !aligned16(d_x) || !grads_ok(grads))
     return LYNX_ERR_INVALID_ARG;
-  if (L->book.state != 1) return LYNX_ERR_STATE;
+  if (L->book.state != 1 || lacks_sequences(L)) return LYNX_ERR_STATE;
   return two_pass(L, static_cast<hipStream_t>(hip_stream),
                   [&](Ctx& cx) { return backward_pass(cx, d_out, d_x, grads); });
 }

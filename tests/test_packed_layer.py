@@ -100,6 +100,18 @@ def test_order_of_calls_and_refusals():
     assert B._lib.lynx_layer_set_position_bias(None, 0, None, None, None) == B.LYNX_ERR_INVALID_ARG
 
 
+def test_a_dry_run_that_is_switched_off_between_its_passes():
+    h = layer()
+    B.lynx_layer_set_dry_run(h, True)
+    B.lynx_layer_forward(h, FAKE, FAKE, 1)
+    B.lynx_layer_set_dry_run(h, False)
+    live = B.lynx_layer_live_mask(h)
+    assert status(B.lynx_recompute, h, B.LYNX_SEG_ALL_MISSING) == B.LYNX_ERR_STATE
+    assert status(B.lynx_layer_backward, h, FAKE, FAKE, {n: FAKE for n in B.PARAM_FIELDS}) == B.LYNX_ERR_STATE
+    assert B.lynx_layer_live_mask(h) == live
+    B.lynx_layer_destroy(h)
+
+
 def test_the_workspace_takes_any_sequences_and_bias():
     """The room that backward keeps covers what the kernels' own call asks for."""
     for seq, b, heads in ((8, 1, 1), (72, 2, 2), (2048, 8, 5), (8192, 4, 3)):
