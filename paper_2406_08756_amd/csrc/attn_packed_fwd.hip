@@ -383,12 +383,14 @@ hipError_t launch_fwd(const PackedAttn& g, hipStream_t st) {
 
 }  // namespace
 
-// Workgroups of 128 rows that the card takes at a time; with fewer, 32 rows each go faster (2048 tokens of 5 heads, 85: 25 us
-// against 62; 139 tiles of 5 heads, 695: 96 us, with 32 rows each 103).
-constexpr size_t kRowGroups = 512;
-// Of 128 keys it takes as many for heads of up to 64, half for wider ones.  They differ more in size, and it takes two rounds
-// of them to even that out (heads of 64, 576 of them: 361 us, with 32 keys each 194; 1088: 113 and 126; heads of 128, 695:
-// 170 and 215).  And sequences that are shorter than a tile leave most of one empty (256 of 32 tokens on average: 43 us and 31).
+// So many workgroups of 128 rows keep the card busy; with fewer, 32 rows each go faster, although each reads K and V for itself
+// (forward, 5 heads of 128, 85: 25 us against 62, 245: 42 and 54; 445: 57 and 48; 8 heads of 64, 392: 32 and 43, 5, 445: 33 and
+// 35, 490: 22 and 19).  dQ with a bias changes earlier for heads of 128, whose 32 rows have a CU to themselves (245: 112 and
+// 94, 376: 227 and 141, 445: 161 and 84, but 170, one sequence of 3000 among them: 83 and 125).
+constexpr size_t kRowGroups = 400, kWideBiasRowGroups = 208;
+// Workgroups of 128 keys are enough at 512 for heads of up to 64, at half of that for wider ones.  They differ more in size,
+// and it takes two rounds of them to even that out (heads of 64, 576 of them: 361 us, with 32 keys each 194; 1088: 113 and
+// 126; heads of 128, 695: 170 and 215).  And sequences that are shorter than a tile leave most of one empty (256 of 32 tokens on average: 43 us and 31).
 constexpr size_t key_groups(int d) { return d <= 64 ? 512 : 256; }
 constexpr int kShort = 96;
 // As many heads of a group as are a power of two, up to 8; fewer where their biases by distance would take more than 10 KB of
@@ -397,8 +399,9 @@ void attn_packed_choose(int dtype, PackedAttn* g) {
   const int group = g->heads / g->kv_heads;
   g->pack = 0;
   while (g->pack < 3 && (group >> g->pack) % 2 == 0 && (g->buckets == 0 || table_stride(*g) << (g->pack + 1) <= 2560)) ++g->pack;
-  g->split_fwd = attn_packed_row_slots(*g, false) * (g->heads >> g->pack) < kRowGroups;
-  g->split_rows = g->split_fwd && attn_packed_split_rows_fit(dtype, *g);
+  const size_t row_groups = attn_packed_row_slots(*g, false) * (g->heads >> g->pack);
+  g->split_fwd = row_groups < kRowGroups;
+  g->split_rows = row_groups < (g->buckets > 0 && g->d > 64 ? kWideBiasRowGroups : kRowGroups) && attn_packed_split_rows_fit(dtype, *g);
   g->split_keys = 0;
   g->split_keys = attn_packed_key_slots(*g) * g->kv_heads < 2 * key_groups(g->d) || g->tokens / g->sequences < kShort;
   g->row_slots = static_cast<int>(attn_packed_row_slots(*g, g->split_rows));

@@ -1,5 +1,5 @@
 """Packed attention with many heads: launches of enough workgroups that each takes 128 rows or keys, whose waves share tiles
-(fewer give every wave tiles of its own).  Rows: (tokens << pack) / 128 + sequences tiles times heads >> pack are 512 or more;
+(fewer give every wave tiles of its own).  Rows: (tokens << pack) / 128 + sequences tiles times heads >> pack are 400 or more;
 keys: tokens / 128 + sequences tiles times kv_heads are 1024 (head_dim <= 64) or 512 or more, of 96 tokens a sequence or more."""
 import math
 
