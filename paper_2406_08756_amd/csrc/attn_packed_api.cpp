@@ -45,7 +45,7 @@ lynx_status make_args(const lynx_attention_config* c, bool backward, PackedAttn*
 
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 size_t delta_bytes(const PackedAttn& g) { return round_up(static_cast<size_t>(g.heads) * g.tokens * sizeof(float)); }
-size_t partials_bytes(const PackedAttn& g) { return round_up(lynx::attn_packed_row_slots(g, g.split_rows) * g.heads * g.buckets * sizeof(float)); }
+size_t partials_bytes(const PackedAttn& g) { return round_up(static_cast<size_t>(g.row_slots) * g.heads * g.buckets * sizeof(float)); }
 
 // (a b)^.. in whole numbers, for the borders of the buckets: at most 64 factors below 2^12
 struct Whole {

@@ -930,11 +930,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP == 64 ? 2 : 1) void 
 
 template <typename T, int DP, bool BIAS>
 hipError_t launch_bwd(const PackedAttn& g, hipStream_t st) {
+  PackedAttn rows = g;
+  rows.pack = g.pack_rows;
   const size_t table = BIAS ? static_cast<size_t>(table_floats(g)) * sizeof(float) : 0;
-  const size_t by_row = table + (BIAS ? kWaves * by_distance_floats(g) * sizeof(float) : 0);
-  const size_t row_groups = static_cast<size_t>(g.row_slots) * (g.heads >> g.pack), key_groups = static_cast<size_t>(g.key_slots) * g.kv_heads;
-  hipError_t e = g.split_rows ? launch_packed<attn_packed_rows_kernel<T, DP, BIAS, true>>(row_groups, Rows<T, DP, BIAS, true>::kLds + by_row, g, st)
-                              : launch_packed<attn_packed_rows_kernel<T, DP, BIAS, false>>(row_groups, Rows<T, DP, BIAS, false>::kLds + by_row, g, st);
+  const size_t by_row = BIAS ? (table_floats(rows) + kWaves * by_distance_floats(rows)) * sizeof(float) : 0;
+  const size_t row_groups = static_cast<size_t>(g.row_slots) * (g.heads >> rows.pack), key_groups = static_cast<size_t>(g.key_slots) * g.kv_heads;
+  hipError_t e = g.split_rows ? launch_packed<attn_packed_rows_kernel<T, DP, BIAS, true>>(row_groups, Rows<T, DP, BIAS, true>::kLds + by_row, rows, st)
+                              : launch_packed<attn_packed_rows_kernel<T, DP, BIAS, false>>(row_groups, Rows<T, DP, BIAS, false>::kLds + by_row, rows, st);
   if (e != hipSuccess) return e;
   // (behind the key tiles a workgroup per head joins the table's gradient: a launch of its own was 4 us)
   const size_t groups = key_groups + (BIAS ? g.heads : 0);

@@ -393,23 +393,32 @@ constexpr size_t kRowGroups = 400, kWideBiasRowGroups = 208;
 // 126; heads of 128, 695: 170 and 215).  And sequences that are shorter than a tile leave most of one empty (256 of 32 tokens on average: 43 us and 31).
 constexpr size_t key_groups(int d) { return d <= 64 ? 512 : 256; }
 constexpr int kShort = 96;
-// As many heads of a group as are a power of two, up to 8; fewer where their biases by distance would take more than 10 KB of
-// LDS, so that with four times that for the gradient's sums and the tiles of fp32 a workgroup has what it needs.
+// As many heads of a group as are a power of two, up to 8; fewer where their biases by distance would take more than `floats`
+// of LDS.  10 KB leave a workgroup what it needs.  The sums of the bias's gradient take four times that: where heads are wider
+// than 64, half of it for dQ, so that two workgroups share a CU (seven sequences of 1500, 16 heads on 2 of 128: 288 us with 8
+// heads to a tile and 185 with 4, but forward 111 and 116, dK and dV 352 and 377).
+static int heads_together(const PackedAttn& g, int floats) {
+  const int group = g.heads / g.kv_heads;
+  int pack = 0;
+  while (pack < 3 && (group >> pack) % 2 == 0 && (g.buckets == 0 || table_stride(g) << (pack + 1) <= floats)) ++pack;
+  return pack;
+}
 void attn_packed_choose(int dtype, PackedAttn* g) {
-  const int group = g->heads / g->kv_heads;
-  g->pack = 0;
-  while (g->pack < 3 && (group >> g->pack) % 2 == 0 && (g->buckets == 0 || table_stride(*g) << (g->pack + 1) <= 2560)) ++g->pack;
-  const size_t row_groups = attn_packed_row_slots(*g, false) * (g->heads >> g->pack);
-  g->split_fwd = row_groups < kRowGroups;
-  g->split_rows = row_groups < (g->buckets > 0 && g->d > 64 ? kWideBiasRowGroups : kRowGroups) && attn_packed_split_rows_fit(dtype, *g);
+  const auto row_groups = [&](const PackedAttn& x) { return attn_packed_row_slots(x, false) * (x.heads >> x.pack); };
+  g->pack = heads_together(*g, 2560);
+  g->pack_rows = heads_together(*g, g->d > 64 ? 1280 : 2560);
+  g->split_fwd = row_groups(*g) < kRowGroups;
+  PackedAttn rows = *g;
+  rows.pack = g->pack_rows;
+  g->split_rows = row_groups(rows) < (g->buckets > 0 && g->d > 64 ? kWideBiasRowGroups : kRowGroups) && attn_packed_split_rows_fit(dtype, rows);
+  g->row_slots = static_cast<int>(attn_packed_row_slots(rows, g->split_rows));
   g->split_keys = 0;
   g->split_keys = attn_packed_key_slots(*g) * g->kv_heads < 2 * key_groups(g->d) || g->tokens / g->sequences < kShort;
-  g->row_slots = static_cast<int>(attn_packed_row_slots(*g, g->split_rows));
   g->key_slots = static_cast<int>(attn_packed_key_slots(*g));
 }
 bool attn_packed_fits(const PackedAttn& g) {
-  const long long subs = g.heads >> g.pack, fwd = static_cast<long long>(attn_packed_row_slots(g, g.split_fwd)) * subs;
-  const long long rows = static_cast<long long>(attn_packed_row_slots(g, g.split_rows)) * subs, keys = static_cast<long long>(attn_packed_key_slots(g)) * g.kv_heads + g.heads;
+  const long long fwd = static_cast<long long>(attn_packed_row_slots(g, g.split_fwd)) * (g.heads >> g.pack);
+  const long long rows = static_cast<long long>(g.row_slots) * (g.heads >> g.pack_rows), keys = static_cast<long long>(g.key_slots) * g.kv_heads + g.heads;
   return fits_grid(fwd, kThreads) && fits_grid(rows, kThreads) && fits_grid(keys, kThreads);
 }
 size_t attn_packed_row_slots(const PackedAttn& g, bool split) {

@@ -246,6 +246,7 @@ struct PackedAttn {
   int sequences, tokens, heads, kv_heads, d;
   int pack;                // log2 of the query heads whose rows share a tile
   int split_fwd, split_rows, split_keys;  // 32 rows (keys) per workgroup instead of 128: forward and the two backward kernels
+  int pack_rows;           // the same for dQ, whose kernel has the bias's gradient in LDS
   int row_slots, key_slots;  // tiles that the backward launches have room for
   float scale;
   int buckets, far;        // far: the distance from which on the last bucket holds, at least 1

@@ -31,6 +31,7 @@ SHAPES = [
     (64, 64, 104, FEWER, None, dict(fused=False, pad=16)),
     (128, 64, 128, FEWER, None, {}),
     (256, 64, 72, FEWER, (32, 128), dict(tail=9)),
+    (128, 16, 104, FEWER, (32, 128), {}),  # (dQ with fewer heads to a tile than the others)
     (5, 5, 64, [96 + 7 * (i % 5) for i in range(130)], (32, 128), {}),  # (more sequences than are ordered by size)
     (5, 5, 96, [96 + 7 * (i % 5) for i in range(130)], None, {}),
     (6, 1, 48, [3] * 520 + [0] + [70, 1], (9, 2048), {}),  # (rows alone are enough)
